@@ -299,6 +299,49 @@ int32_t dion_debug_checks(void);
 /* Frees the plan's workspace (synchronizes the device first).  NULL is a no-op. */
 void dion_plan_destroy(dion_plan *plan);
 
+/* ------------------------------------------------------------------------------------------
+ * Language-model operators: the work of a GPT training step around its matrices.  The token
+ * embedding with its gradient, the norm and rotation of queries and keys with its gradient, and
+ * the loss of distillation from a teacher's top logits with its gradient.  Their matrix gradients
+ * are what dion_step takes; none of them is part of the paper.
+ *
+ * As everywhere here: tensors are device pointers of the caller, leading dimensions and strides
+ * count elements, a host-detectable error returns a status and enqueues nothing, and a call only
+ * enqueues work on `stream` (a cudaStream_t; NULL = legacy default stream): it neither blocks nor
+ * allocates.  A plan belongs to the device that was current when it was created and must not be
+ * used on two streams at the same time; the calls without a plan run on the current device.
+ * Pointers need the alignment of their element only; rows that begin on 16 bytes are read and
+ * written with wide accesses.  Sums, norms and softmax statistics are held in fp32, and a result
+ * is rounded to its type once.  Results are the same from call to call, bit for bit. */
+
+/* Element type of an array of indices (tokens, positions, labels). */
+enum { DION_INDEX_INT32 = 0, DION_INDEX_INT64 = 1 };
+
+/* Token embedding.  A plan for a table of `vocab` rows of `dim` elements holds the workspace of
+ * the gradient's sort for calls of up to max_tokens tokens (16 bytes per token and a few MB).
+ *   lookup:    out[i] = scale * table[tokens[i]]
+ *   gradient:  table_grad[v] = scale * sum of grad[i] over the i with tokens[i] = v; rows of tokens
+ *              that do not occur become zeros.  accumulate != 0: the sums are added to table_grad
+ *              instead and other rows are neither read nor written (micro-batches, tied tables).
+ * A token outside [0, vocab) (padding) gives a row of zeros and no gradient.  The sum of a row runs
+ * over sorted tokens in the order of their positions, split at points that depend on the sizes and
+ * the tokens alone.  tokens: num_tokens contiguous indices; table, out, grad, table_grad: row-major
+ * with leading dimensions ld >= dim, types DION_DTYPE_* each on its own.  Outputs must not overlap
+ * inputs.
+ * Errors: INVALID_ARG (NULL pointer, size < 0 or ld < dim, unknown type, scale not finite,
+ * num_tokens > max_tokens in the gradient), UNSUPPORTED (vocab, max_tokens or dim of 2^30 or more),
+ * ALIGNMENT (pointer not a multiple of its element), CUDA. */
+typedef struct dion_embed_plan dion_embed_plan;
+dion_status dion_embed_plan_create(int64_t vocab, int64_t dim, int64_t max_tokens, dion_embed_plan **out);
+dion_status dion_embed_lookup(dion_embed_plan *plan, const void *tokens, int32_t token_dtype, int64_t num_tokens,
+                              const void *table, int32_t table_dtype, int64_t ldt, float scale, void *out,
+                              int32_t out_dtype, int64_t ldo, void *stream);
+dion_status dion_embed_gradient(dion_embed_plan *plan, const void *tokens, int32_t token_dtype, int64_t num_tokens,
+                                const void *grad, int32_t grad_dtype, int64_t ldg, float scale, void *table_grad,
+                                int32_t table_grad_dtype, int64_t ldd, int32_t accumulate, void *stream);
+/* Frees the plan's workspace (synchronizes the device first).  NULL is a no-op. */
+void dion_embed_plan_destroy(dion_embed_plan *plan);
+
 /* Static description of a status code. */
 const char *dion_status_string(dion_status status);
 

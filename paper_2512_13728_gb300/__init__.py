@@ -2,7 +2,8 @@
 
 ``native`` is the ctypes binding of include/curvadion.h (same names as the C entry points).
 ``Plan`` marshals torch CUDA tensors into ``dion_layer`` structs and owns the per-step
-device outputs; torch is used only for device memory and streams.
+device outputs; torch is used only for device memory and streams.  ``lm`` does the same for the
+language-model operators around the matrices (``EmbedPlan``).
 """
 from __future__ import annotations
 
@@ -13,6 +14,18 @@ from .native import (DION_DTYPE_BF16, DION_DTYPE_FP32, DION_GATE_ALWAYS, DION_GA
                      DION_GATE_PER_LAYER, DION_GATE_SCHEDULED, DION_PHASE_NORMS, DION_PHASE_ORTHO,
                      DION_PHASE_POWER, DION_PHASE_UPDATE, DION_PREC_BF16, DION_PREC_BF16X3,
                      DION_PREC_FP32, DionError, dion_hparams, dion_layer)
+
+_LM = ("EmbedPlan",)
+
+
+def __getattr__(name: str):
+    """The operators of ``lm``, which imports torch, on first use."""
+    if name in _LM:
+        from . import lm
+
+        return getattr(lm, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+
 
 
 class _DeviceRange:

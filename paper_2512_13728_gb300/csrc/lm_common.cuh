@@ -1,0 +1,123 @@
+// Shared by the language-model operators (embedding, query/key norm with rotation, distillation):
+// element types, vectors of up to 16 bytes, launches and argument checks.
+#pragma once
+
+#include "../../include/curvadion.h"
+#include "common.cuh"
+
+namespace cd {
+namespace lm {
+
+// V elements of a row as fp32 values.  The address is a multiple of min(16, V * sizeof(T)) bytes.
+template <class T, int V>
+__device__ __forceinline__ void load_vec(const T *p, float (&v)[V]) {
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(p + i);
+        v[i] = x.x, v[i + 1] = x.y, v[i + 2] = x.z, v[i + 3] = x.w;
+      }
+    } else if constexpr (V == 2) {
+      const float2 x = *reinterpret_cast<const float2 *>(p);
+      v[0] = x.x, v[1] = x.y;
+    } else {
+      v[0] = *p;
+    }
+  } else {
+    if constexpr (V == 8) {
+      const uint4 x = *reinterpret_cast<const uint4 *>(p);
+      const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    } else if constexpr (V == 4) {
+      const uint2 x = *reinterpret_cast<const uint2 *>(p);
+      v[0] = __uint_as_float(x.x << 16), v[1] = __uint_as_float(x.x & 0xffff0000u);
+      v[2] = __uint_as_float(x.y << 16), v[3] = __uint_as_float(x.y & 0xffff0000u);
+    } else if constexpr (V == 2) {
+      const uint32_t x = *reinterpret_cast<const uint32_t *>(p);
+      v[0] = __uint_as_float(x << 16), v[1] = __uint_as_float(x & 0xffff0000u);
+    } else {
+      v[0] = __bfloat162float(*p);
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&b);
+}
+
+// The one rounding of an output: fp32 results go to bf16 with round-to-nearest-even here.
+template <class T, int V>
+__device__ __forceinline__ void store_vec(T *p, const float (&v)[V]) {
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    } else if constexpr (V == 2) {
+      *reinterpret_cast<float2 *>(p) = make_float2(v[0], v[1]);
+    } else {
+      *p = v[0];
+    }
+  } else {
+    if constexpr (V == 8)
+      *reinterpret_cast<uint4 *>(p) =
+          make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    else if constexpr (V == 4)
+      *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+    else if constexpr (V == 2)
+      *reinterpret_cast<uint32_t *>(p) = pack_bf16(v[0], v[1]);
+    else
+      *p = __float2bfloat16_rn(v[0]);
+  }
+}
+
+// An index of either width; the caller bounds it.
+__device__ __forceinline__ int64_t load_index(const void *p, int32_t dtype, int64_t i) {
+  return dtype == DION_INDEX_INT64 ? static_cast<const int64_t *>(p)[i] : (int64_t)static_cast<const int32_t *>(p)[i];
+}
+
+inline bool is_dtype(int32_t d) { return d == DION_DTYPE_FP32 || d == DION_DTYPE_BF16; }
+inline bool is_index(int32_t d) { return d == DION_INDEX_INT32 || d == DION_INDEX_INT64; }
+inline int element_bytes(int32_t d) { return d == DION_DTYPE_FP32 ? 4 : 2; }
+inline bool aligned_to(const void *p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
+
+// Launches with the same chaining as a step's kernels (common.cuh) and returns the launch's own
+// status.  cluster > 1: that many consecutive blocks form a cluster.
+template <class... P, class... A>
+inline cudaError_t launch(void (*kernel)(P...), int64_t grid, int block, size_t smem, cudaStream_t s, int cluster, A &&...args) {
+  cudaLaunchAttribute at[2]{};
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
+// Makes a plan's device current for the duration of a call.
+struct OnDevice {
+  int prev = -1;
+  bool ok = true;
+  explicit OnDevice(int dev) {
+    if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
+    if (prev == dev)
+      prev = -1;  // nothing to put back
+    else
+      ok = cudaSetDevice(dev) == cudaSuccess;
+  }
+  ~OnDevice() {
+    if (prev >= 0) cudaSetDevice(prev);
+  }
+};
+
+}  // namespace lm
+}  // namespace cd

@@ -30,6 +30,9 @@ DION_GATE_SCHEDULED = 3
 DION_DTYPE_FP32 = 0
 DION_DTYPE_BF16 = 1
 
+DION_INDEX_INT32 = 0
+DION_INDEX_INT64 = 1
+
 DION_PREC_FP32 = 0
 DION_PREC_BF16 = 1
 DION_PREC_BF16X3 = 2
@@ -46,7 +49,8 @@ EXPORTED = ("dion_plan_create", "dion_step", "dion_get_device_status", "dion_pla
             "dion_timing_enable", "dion_timing_read", "dion_buffer_norms_noalloc", "dion_plan_destroy",
             "dion_status_string", "dion_abi_version", "dion_plan_enable_host_gradients", "dion_step_host",
             "dion_lr_schedule", "dion_rank_for", "dion_plan_set_wait_limit", "dion_step_phase", "dion_plan_exchange",
-            "dion_plan_check_guards", "dion_debug_checks")
+            "dion_plan_check_guards", "dion_debug_checks", "dion_embed_plan_create", "dion_embed_lookup",
+            "dion_embed_gradient", "dion_embed_plan_destroy")
 
 DION_ABI_VERSION = 3
 DION_NOALLOC_MAX_LAYERS = 256
@@ -127,6 +131,15 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.dion_debug_checks.restype = C.c_int32
     lib.dion_plan_set_wait_limit.argtypes = [P, C.c_int64]
     lib.dion_plan_set_wait_limit.restype = C.c_int
+    I32, I64, F32 = C.c_int32, C.c_int64, C.c_float
+    lib.dion_embed_plan_create.argtypes = [I64, I64, I64, C.POINTER(P)]
+    lib.dion_embed_plan_create.restype = C.c_int
+    lib.dion_embed_lookup.argtypes = [P, P, I32, I64, P, I32, I64, F32, P, I32, I64, P]
+    lib.dion_embed_lookup.restype = C.c_int
+    lib.dion_embed_gradient.argtypes = [P, P, I32, I64, P, I32, I64, F32, P, I32, I64, I32, P]
+    lib.dion_embed_gradient.restype = C.c_int
+    lib.dion_embed_plan_destroy.argtypes = [P]
+    lib.dion_embed_plan_destroy.restype = None
     lib.dion_plan_destroy.argtypes = [P]
     lib.dion_plan_destroy.restype = None
     lib.dion_status_string.argtypes = [C.c_int]
@@ -285,3 +298,35 @@ def dion_plan_set_wait_limit(plan: int, limit_ns: int) -> None:
 def dion_plan_destroy(plan: int) -> None:
     if plan:
         load().dion_plan_destroy(C.c_void_p(plan))
+
+
+def dion_embed_plan_create(vocab: int, dim: int, max_tokens: int) -> int:
+    out = C.c_void_p()
+    st = load().dion_embed_plan_create(vocab, dim, max_tokens, C.byref(out))
+    if st != DION_OK:
+        raise DionError(st, "dion_embed_plan_create")
+    return out.value
+
+
+def dion_embed_lookup(plan: int, tokens: int, token_dtype: int, num_tokens: int, table: int, table_dtype: int, ldt: int,
+                      scale: float, out: int, out_dtype: int, ldo: int, stream: int) -> None:
+    """All pointers are device addresses (ints)."""
+    st = load().dion_embed_lookup(plan, tokens, token_dtype, num_tokens, table, table_dtype, ldt, scale, out, out_dtype,
+                                  ldo, stream)
+    if st != DION_OK:
+        raise DionError(st, "dion_embed_lookup")
+
+
+def dion_embed_gradient(plan: int, tokens: int, token_dtype: int, num_tokens: int, grad: int, grad_dtype: int, ldg: int,
+                        scale: float, table_grad: int, table_grad_dtype: int, ldd: int, accumulate: int,
+                        stream: int) -> None:
+    """All pointers are device addresses (ints)."""
+    st = load().dion_embed_gradient(plan, tokens, token_dtype, num_tokens, grad, grad_dtype, ldg, scale, table_grad,
+                                    table_grad_dtype, ldd, accumulate, stream)
+    if st != DION_OK:
+        raise DionError(st, "dion_embed_gradient")
+
+
+def dion_embed_plan_destroy(plan: int) -> None:
+    if plan:
+        load().dion_embed_plan_destroy(plan)
