@@ -312,7 +312,8 @@ void dion_plan_destroy(dion_plan *plan);
  * used on two streams at the same time; the calls without a plan run on the current device.
  * Pointers need the alignment of their element only; rows that begin on 16 bytes are read and
  * written with wide accesses.  Sums, norms and softmax statistics are held in fp32, and a result
- * is rounded to its type once.  Results are the same from call to call, bit for bit. */
+ * is rounded to its type once.  Results are the same from call to call, bit for bit, for the same
+ * sizes, strides and alignment. */
 
 /* Element type of an array of indices (tokens, positions, labels). */
 enum { DION_INDEX_INT32 = 0, DION_INDEX_INT64 = 1 };
@@ -341,6 +342,79 @@ dion_status dion_embed_gradient(dion_embed_plan *plan, const void *tokens, int32
                                 int32_t table_grad_dtype, int64_t ldd, int32_t accumulate, void *stream);
 /* Frees the plan's workspace (synchronizes the device first).  NULL is a no-op. */
 void dion_embed_plan_destroy(dion_embed_plan *plan);
+
+/* Norm and rotation of queries and keys, one pass.  For each head x of head_dim elements of each
+ * token, with the weights w of its kind (fp32, head_dim; NULL = ones):
+ *   r = 1 / sqrt(mean(x^2) + eps),  u = w * (r x),
+ *   pairs (a, b) of u's first rotary_dim elements turned by angle_j = position * inv_freq[j]:
+ *   a' = a cos - b sin,  b' = b cos + a sin,  j < rotary_dim / 2; the other elements pass.
+ * Pair j is (j, j + rotary_dim / 2), or (2 j, 2 j + 1) with interleaved != 0.  inv_freq (host,
+ * rotary_dim / 2 doubles) is copied; NULL: theta^(-2 j / rotary_dim).  Angles are reduced exactly
+ * (a position times a 64-bit fraction of a turn), so positions have no limit and no table is kept.
+ *   backward: from the gradients of the outputs, those of q, k (recomputing r from q, k) and, where
+ *   the pointers are not NULL, of the weights (fp32, head_dim each; overwritten).
+ * Sizes: even head_dim in [2, 256], even rotary_dim in [0, head_dim].  Heads of q and of k may differ
+ * in number; kv_heads = 0 leaves k out (its dion_heads may be NULL then).  A tensor is given by
+ * dion_heads: element (b, t, h, d) is at data[b * batch_stride + t * token_stride + h * head_stride + d].
+ * positions: index (b, t) at positions[b * position_batch_stride + t]; NULL: the position of token t is t.
+ * An output may be its own input (the same dion_heads: in place); otherwise they must not overlap.
+ * Errors: INVALID_ARG (NULL pointer, size out of range, unknown type, eps < 0 or not finite, theta <= 0),
+ * UNSUPPORTED (head_dim > 256, or 2^40 elements or more), ALIGNMENT (pointer not a multiple of its
+ * element), CUDA. */
+typedef struct dion_qknorm_plan dion_qknorm_plan;
+typedef struct {
+  void *data;
+  int64_t batch_stride, token_stride, head_stride;
+} dion_heads;
+typedef struct {
+  int64_t batch, tokens;    /* sequences, tokens of each */
+  int32_t heads, kv_heads;  /* of q, of k */
+  int32_t dtype;            /* DION_DTYPE_* of q, k, their outputs and gradients */
+  int32_t position_dtype;   /* DION_INDEX_* */
+  const void *positions;
+  int64_t position_batch_stride;
+} dion_qk_shape;
+dion_status dion_qknorm_plan_create(int32_t head_dim, int32_t rotary_dim, int32_t interleaved, double theta,
+                                    const double *inv_freq, float eps, dion_qknorm_plan **out);
+dion_status dion_qknorm_forward(dion_qknorm_plan *plan, const dion_qk_shape *shape, const dion_heads *q,
+                                const dion_heads *k, const float *wq, const float *wk, const dion_heads *q_out,
+                                const dion_heads *k_out, void *stream);
+dion_status dion_qknorm_backward(dion_qknorm_plan *plan, const dion_qk_shape *shape, const dion_heads *gq,
+                                 const dion_heads *gk, const dion_heads *q, const dion_heads *k, const float *wq,
+                                 const float *wk, const dion_heads *dq, const dion_heads *dk, float *dwq, float *dwk,
+                                 void *stream);
+/* Frees the plan's workspace (synchronizes the device first).  NULL is a no-op. */
+void dion_qknorm_plan_destroy(dion_qknorm_plan *plan);
+
+/* Distillation from a teacher's top logits.  Row i has logits z (vocab elements), the teacher's
+ * `top` entries (id_k, t_k), a label y and a weight w (NULL weights: ones):
+ *   p = softmax(t / T) over the present entries,  q = softmax(z / T),  q1 = softmax(z)
+ *   loss_i = w [ (1 - hard) T^2 sum_k p_k (log p_k - log q[id_k])  -  hard log q1[y] ]
+ *   grad_i = d loss_i / d z = w [ (1 - hard) T (q - sum_k p_k e[id_k])  +  hard (q1 - e[y]) ]
+ * An entry whose id is outside [0, vocab) or whose t is -infinity is absent (ragged lists are padded
+ * with -1); a row without present entries has no first term, a row whose label is outside [0, vocab)
+ * no second one.  hard = 0 reads no labels (NULL allowed), hard = 1 no teacher entries (NULL allowed).
+ * An id that comes twice counts twice.  A row of weight 0 is not read: its loss is 0 and its gradient
+ * zeros, whatever its logits hold.  Logits of -infinity have probability 0.
+ * loss: fp32, rows.  grad: type of the logits, may be the logits' own memory (same pointer and ld).
+ * Errors: INVALID_ARG (NULL pointer, size < 0, vocab < 1, ld < columns, unknown type, temperature <= 0 or
+ * not finite, hard outside [0, 1], index or label pointer missing), UNSUPPORTED (top >
+ * DION_DISTILL_MAX_TOP; vocab > DION_DISTILL_MAX_VOCAB; more than 2^30 rows), ALIGNMENT (pointer not a multiple of its
+ * element), CUDA. */
+#define DION_DISTILL_MAX_TOP 1024
+#define DION_DISTILL_MAX_VOCAB 393216
+typedef struct {
+  int64_t rows, vocab, top;
+  const void *logits;  int64_t ld;
+  const void *ids;     int64_t ld_ids;
+  const void *teacher; int64_t ld_teacher;
+  const void *labels;
+  const float *weights;
+  int32_t dtype, id_dtype, teacher_dtype, label_dtype;
+  float temperature, hard;
+} dion_distill;
+dion_status dion_distill_loss(const dion_distill *args, float *loss, void *stream);
+dion_status dion_distill_loss_grad(const dion_distill *args, float *loss, void *grad, int64_t ldg, void *stream);
 
 /* Static description of a status code. */
 const char *dion_status_string(dion_status status);

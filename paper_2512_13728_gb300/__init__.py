@@ -3,7 +3,8 @@
 ``native`` is the ctypes binding of include/curvadion.h (same names as the C entry points).
 ``Plan`` marshals torch CUDA tensors into ``dion_layer`` structs and owns the per-step
 device outputs; torch is used only for device memory and streams.  ``lm`` does the same for the
-language-model operators around the matrices (``EmbedPlan``).
+language-model operators around the matrices (``EmbedPlan``, ``QKNormPlan``, ``distill_loss``,
+``distill_loss_grad``).
 """
 from __future__ import annotations
 
@@ -15,7 +16,7 @@ from .native import (DION_DTYPE_BF16, DION_DTYPE_FP32, DION_GATE_ALWAYS, DION_GA
                      DION_PHASE_POWER, DION_PHASE_UPDATE, DION_PREC_BF16, DION_PREC_BF16X3,
                      DION_PREC_FP32, DionError, dion_hparams, dion_layer)
 
-_LM = ("EmbedPlan",)
+_LM = ("EmbedPlan", "QKNormPlan", "distill_loss", "distill_loss_grad")
 
 
 def __getattr__(name: str):

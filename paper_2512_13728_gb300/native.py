@@ -50,11 +50,14 @@ EXPORTED = ("dion_plan_create", "dion_step", "dion_get_device_status", "dion_pla
             "dion_status_string", "dion_abi_version", "dion_plan_enable_host_gradients", "dion_step_host",
             "dion_lr_schedule", "dion_rank_for", "dion_plan_set_wait_limit", "dion_step_phase", "dion_plan_exchange",
             "dion_plan_check_guards", "dion_debug_checks", "dion_embed_plan_create", "dion_embed_lookup",
-            "dion_embed_gradient", "dion_embed_plan_destroy")
+            "dion_embed_gradient", "dion_embed_plan_destroy", "dion_qknorm_plan_create", "dion_qknorm_forward",
+            "dion_qknorm_backward", "dion_qknorm_plan_destroy", "dion_distill_loss", "dion_distill_loss_grad")
 
 DION_ABI_VERSION = 3
 DION_NOALLOC_MAX_LAYERS = 256
 DION_NOALLOC_MAX_TILES = 65536
+DION_DISTILL_MAX_TOP = 1024
+DION_DISTILL_MAX_VOCAB = 393216
 
 
 class dion_layer(C.Structure):
@@ -76,6 +79,25 @@ class dion_hparams(C.Structure):
         ("gate_mode", C.c_int32), ("period", C.c_int32), ("step", C.c_int64),
         ("weight_decay", C.c_float),
     ]
+
+
+class dion_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
+
+
+class dion_qk_shape(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("tokens", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("dtype", C.c_int32), ("position_dtype", C.c_int32), ("positions", C.c_void_p),
+                ("position_batch_stride", C.c_int64)]
+
+
+class dion_distill(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("top", C.c_int64), ("logits", C.c_void_p), ("ld", C.c_int64),
+                ("ids", C.c_void_p), ("ld_ids", C.c_int64), ("teacher", C.c_void_p), ("ld_teacher", C.c_int64),
+                ("labels", C.c_void_p), ("weights", C.c_void_p), ("dtype", C.c_int32), ("id_dtype", C.c_int32),
+                ("teacher_dtype", C.c_int32), ("label_dtype", C.c_int32), ("temperature", C.c_float),
+                ("hard", C.c_float)]
 
 
 class DionError(RuntimeError):
@@ -140,6 +162,19 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.dion_embed_gradient.restype = C.c_int
     lib.dion_embed_plan_destroy.argtypes = [P]
     lib.dion_embed_plan_destroy.restype = None
+    H = C.POINTER(dion_heads)
+    lib.dion_qknorm_plan_create.argtypes = [I32, I32, I32, C.c_double, C.POINTER(C.c_double), F32, C.POINTER(P)]
+    lib.dion_qknorm_plan_create.restype = C.c_int
+    lib.dion_qknorm_forward.argtypes = [P, C.POINTER(dion_qk_shape), H, H, P, P, H, H, P]
+    lib.dion_qknorm_forward.restype = C.c_int
+    lib.dion_qknorm_backward.argtypes = [P, C.POINTER(dion_qk_shape), H, H, H, H, P, P, H, H, P, P, P]
+    lib.dion_qknorm_backward.restype = C.c_int
+    lib.dion_qknorm_plan_destroy.argtypes = [P]
+    lib.dion_qknorm_plan_destroy.restype = None
+    lib.dion_distill_loss.argtypes = [C.POINTER(dion_distill), P, P]
+    lib.dion_distill_loss.restype = C.c_int
+    lib.dion_distill_loss_grad.argtypes = [C.POINTER(dion_distill), P, P, I64, P]
+    lib.dion_distill_loss_grad.restype = C.c_int
     lib.dion_plan_destroy.argtypes = [P]
     lib.dion_plan_destroy.restype = None
     lib.dion_status_string.argtypes = [C.c_int]
@@ -330,3 +365,44 @@ def dion_embed_gradient(plan: int, tokens: int, token_dtype: int, num_tokens: in
 def dion_embed_plan_destroy(plan: int) -> None:
     if plan:
         load().dion_embed_plan_destroy(plan)
+
+
+def dion_qknorm_plan_create(head_dim: int, rotary_dim: int, interleaved: bool, theta: float, inv_freq, eps: float) -> int:
+    """inv_freq: rotary_dim / 2 floats, or None for the powers of theta."""
+    freq = (C.c_double * len(inv_freq))(*inv_freq) if inv_freq is not None else None
+    out = C.c_void_p()
+    st = load().dion_qknorm_plan_create(head_dim, rotary_dim, 1 if interleaved else 0, theta, freq, eps, C.byref(out))
+    if st != DION_OK:
+        raise DionError(st, "dion_qknorm_plan_create")
+    return out.value
+
+
+def dion_qknorm_forward(plan: int, shape: dion_qk_shape, q, k, wq, wk, q_out, k_out, stream: int) -> None:
+    """q, k, q_out, k_out: dion_heads (k, k_out may be None); wq, wk: device addresses or None."""
+    st = load().dion_qknorm_forward(plan, shape, q, k, wq, wk, q_out, k_out, stream)
+    if st != DION_OK:
+        raise DionError(st, "dion_qknorm_forward")
+
+
+def dion_qknorm_backward(plan: int, shape: dion_qk_shape, gq, gk, q, k, wq, wk, dq, dk, dwq, dwk, stream: int) -> None:
+    """gq, gk, q, k, dq, dk: dion_heads (those of k may be None); the others: device addresses or None."""
+    st = load().dion_qknorm_backward(plan, shape, gq, gk, q, k, wq, wk, dq, dk, dwq, dwk, stream)
+    if st != DION_OK:
+        raise DionError(st, "dion_qknorm_backward")
+
+
+def dion_qknorm_plan_destroy(plan: int) -> None:
+    if plan:
+        load().dion_qknorm_plan_destroy(plan)
+
+
+def dion_distill_loss(args: dion_distill, loss: int, stream: int) -> None:
+    st = load().dion_distill_loss(args, loss, stream)
+    if st != DION_OK:
+        raise DionError(st, "dion_distill_loss")
+
+
+def dion_distill_loss_grad(args: dion_distill, loss: int, grad: int, ldg: int, stream: int) -> None:
+    st = load().dion_distill_loss_grad(args, loss, grad, ldg, stream)
+    if st != DION_OK:
+        raise DionError(st, "dion_distill_loss_grad")
