@@ -359,7 +359,7 @@ void dion_embed_plan_destroy(dion_embed_plan *plan);
  * positions: index (b, t) at positions[b * position_batch_stride + t]; NULL: the position of token t is t.
  * An output may be its own input (the same dion_heads: in place); otherwise they must not overlap.
  * Errors: INVALID_ARG (NULL pointer, size out of range, unknown type, eps < 0 or not finite, theta <= 0),
- * UNSUPPORTED (head_dim > 256, or 2^40 elements or more), ALIGNMENT (pointer not a multiple of its
+ * UNSUPPORTED (head_dim > 256, more than 2048 heads of a kind, or more than 2^40 elements), ALIGNMENT (pointer not a multiple of its
  * element), CUDA. */
 typedef struct dion_qknorm_plan dion_qknorm_plan;
 typedef struct {

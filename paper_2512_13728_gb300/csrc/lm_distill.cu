@@ -1,10 +1,15 @@
 // Distillation from a teacher's top logits: loss, and loss with gradient.
 //
-// Per row, with c = log2(e):  q_j = 2^((z_j - m) c / T) / s_T,  s_T = sum_j 2^((z_j - m) c / T),  m = max z,
-// and the same with T = 1 for the hard labels.  One pass holds the running m, s_T and s_1.  The gradient
-// needs the row again: a row (or, for long ones, its part) stays in shared memory between the two uses,
-// so the logits are read once and the gradient is written once.  A cluster of blocks shares a row that
-// is too long for one block, or rows that are too few to fill the GPU.
+// Per row, with c = log2(e) / T and m = max z:  q_j = 2^(c (z_j - m)) / s,  s = sum_j 2^(c (z_j - m)).  One
+// pass over the row holds the running m and s.  The maximum is taken off before the scaling, so that
+// logits at the end of the type's range (masks of its lowest value) neither overflow nor lose a row.
+// Where the loss has both terms and T is not 1, a second sum at T = 1 runs along.
+//
+// The gradient needs the row again: a row (or, for long ones, each block's part of it) stays in shared
+// memory between the two uses, so the logits are read once and the gradient is written once, and the next
+// row is on its way while this one is worked on.  A thread only ever reads what it copied itself, so a
+// row costs one block barrier, between the sums and the gradient.  One warp of the block does all that
+// belongs to the teacher's entries, a row ahead of the others.
 #include "lm_common.cuh"
 
 #include <algorithm>
@@ -17,11 +22,12 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kPartBytes = 200 * 1024;  // of a row in one block's shared memory
+constexpr int kMaxThreads = 1024;
+constexpr int kLossThreads = 512;
 constexpr int kMaxCluster = 8;
+constexpr size_t kSmemPerSm = 227 * 1024, kSmemPerBlock = 1024;  // of an SM; what the system takes of each block's
+constexpr int kStaticSmem = 2048;                                // at most, of the kernels here
 
 struct Args {
   dion_distill d;
@@ -29,10 +35,16 @@ struct Args {
   void *grad;
   int64_t ldg;
   int32_t cluster, part;  // blocks per row, chunks of 16 bytes per block
+  int32_t buffers;        // rows in shared memory: 2, or 1 where two do not fit
+  int32_t bitmap;         // words
+  float c;                // log2(e) / temperature of the first softmax
+  float k_soft, k_hard;   // (1 - hard) T, hard
+  int32_t soft, hard;     // which terms the loss has
 };
 
-struct Stats {  // running maximum and sums of one set of logits
-  float m, st, s1;
+// Running maximum, sum at the loss's temperature, and where there are two softmaxes the sum at 1.
+struct Stats {
+  float m, s, s1;
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -40,49 +52,111 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-
-// The reference point of an exponential: the maximum, or 0 for a set without finite logits.
-__device__ __forceinline__ float anchor(float m) { return m == -INFINITY ? 0.f : m; }
-
-template <bool SOFT, bool HARD>
-__device__ __forceinline__ Stats merge(const Stats &a, const Stats &b, float ct, float c1) {
-  Stats r;
-  r.m = fmaxf(a.m, b.m);
-  const float at = anchor(r.m);
-  r.st = r.s1 = 0.f;
-  if (SOFT) r.st = a.st * exp2f((a.m - at) * ct) + b.st * exp2f((b.m - at) * ct);
-  if (HARD) r.s1 = a.s1 * exp2f((a.m - at) * c1) + b.s1 * exp2f((b.m - at) * c1);
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float &a, float &b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
 
-// Adds the logits of G chunks to the statistics.
-template <class T, int G, bool SOFT, bool HARD>
-__device__ __forceinline__ void take(const float (&v)[G][16 / sizeof(T)], Stats &s, float ct, float c1) {
-  constexpr int N = 16 / sizeof(T);
-  float m = s.m;
+// What is subtracted in the exponent: the maximum, or 0 for a set without finite logits.
+__device__ __forceinline__ float anchor(float m) { return m == -INFINITY ? 0.f : m; }
+
+template <bool TWO>
+__device__ __forceinline__ Stats merge(const Stats &a, const Stats &b, float c) {
+  Stats r;
+  r.m = fmaxf(a.m, b.m);
+  const float da = a.m - anchor(r.m), db = b.m - anchor(r.m);
+  r.s = a.s * exp2_fast(da * c) + b.s * exp2_fast(db * c);
+  r.s1 = TWO ? a.s1 * exp2_fast(da * kLog2e) + b.s1 * exp2_fast(db * kLog2e) : 0.f;
+  return r;
+}
+template <bool TWO>
+__device__ __forceinline__ Stats merge_lanes(Stats s, float c) {
 #pragma unroll
-  for (int g = 0; g < G; ++g)
+  for (int o = 16; o > 0; o >>= 1) {
+    Stats x;
+    x.m = __shfl_xor_sync(0xffffffffu, s.m, o);
+    x.s = __shfl_xor_sync(0xffffffffu, s.s, o);
+    x.s1 = TWO ? __shfl_xor_sync(0xffffffffu, s.s1, o) : 0.f;
+    s = merge<TWO>(s, x, c);
+  }
+  return s;
+}
+
+// 16 bytes of logits.
+template <class T>
+struct Chunk {
+  static constexpr int N = 16 / sizeof(T);
+  uint4 raw;
+  __device__ __forceinline__ uint64_t pair(int i) const {  // elements 2 i, 2 i + 1 as fp32
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    if constexpr (sizeof(T) == 4) return pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    return pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+  __device__ __forceinline__ float max() const {  // NaN only where every element is
+    if constexpr (sizeof(T) == 4) {
+      return fmaxf(fmaxf(__uint_as_float(raw.x), __uint_as_float(raw.y)), fmaxf(__uint_as_float(raw.z), __uint_as_float(raw.w)));
+    } else {
+      const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+      __nv_bfloat162 h[4];
 #pragma unroll
-    for (int e = 0; e < N; ++e) m = fmaxf(m, v[g][e]);
+      for (int i = 0; i < 4; ++i) h[i] = *reinterpret_cast<const __nv_bfloat162 *>(&w[i]);
+      const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+      return fmaxf(__low2float(m), __high2float(m));
+    }
+  }
+};
+
+// Adds the logits of G chunks to a thread's statistics.
+template <class T, int G, bool TWO>
+__device__ __forceinline__ void take(const Chunk<T> (&v)[G], Stats &s, float c) {
+  float m = v[0].max();
+#pragma unroll
+  for (int g = 1; g < G; ++g) m = fmaxf(m, v[g].max());
   if (m > s.m) {
-    if (SOFT) s.st *= exp2_fast((s.m - m) * ct);
-    if (HARD) s.s1 *= exp2_fast((s.m - m) * c1);
+    s.s *= exp2_fast((s.m - m) * c);
+    if (TWO) s.s1 *= exp2_fast((s.m - m) * kLog2e);
     s.m = m;
   }
   const float at = anchor(s.m);
+  const uint64_t at2 = pack2(-at, -at), c2 = pack2(c, c), l2 = pack2(kLog2e, kLog2e);
+  uint64_t sum = pack2(s.s, 0.f), sum1 = pack2(s.s1, 0.f);
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      if (SOFT) s.st += exp2_fast((v[g][e] - at) * ct);
-      if (HARD) s.s1 += exp2_fast((v[g][e] - at) * c1);
+    for (int i = 0; i < Chunk<T>::N / 2; ++i) {
+      const uint64_t d = add2(v[g].pair(i), at2);
+      float a, b;
+      unpack2(mul2(d, c2), a, b);
+      sum = add2(sum, pack2(exp2_fast(a), exp2_fast(b)));
+      if (TWO) {
+        unpack2(mul2(d, l2), a, b);
+        sum1 = add2(sum1, pack2(exp2_fast(a), exp2_fast(b)));
+      }
     }
-}
-
-__device__ __forceinline__ void copy_16(void *smem, const void *global) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(smem))),
-               "l"(global)
-               : "memory");
+  float a, b;
+  unpack2(sum, a, b);
+  s.s = a + b;
+  unpack2(sum1, a, b);
+  if (TWO) s.s1 = a + b;
 }
 
 template <class T>
@@ -91,263 +165,398 @@ __device__ __forceinline__ float load_one(const T *p) {
   load_vec<T, 1>(p, v);
   return v[0];
 }
-
+template <class T>
+__device__ __forceinline__ void store_one(T *p, float x) {
+  const float v[1] = {x};
+  store_vec<T, 1>(p, v);
+}
 __device__ __forceinline__ float load_any(const void *p, int32_t dtype, int64_t i) {
   return dtype == DION_DTYPE_FP32 ? static_cast<const float *>(p)[i] : load_one(static_cast<const __nv_bfloat16 *>(p) + i);
 }
 
-// One row per cluster.  GRAD: with the gradient.  SOFT, HARD: which terms the loss has.
-template <class T, bool GRAD, bool SOFT, bool HARD>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const Args A) {
-  constexpr int N = 16 / sizeof(T);
-  extern __shared__ uint4 smem[];
-  __shared__ Stats warp_stats[kWarps], block_stats, row_stats;
-  __shared__ float red[kWarps], red2[kWarps];
-  __shared__ int any;
+// One row as a block sees it: chunks of 16 bytes at multiples of 16, of which the block's are [lo, hi).
+template <class T>
+struct Row {
+  static constexpr int N = 16 / sizeof(T);
+  const T *z;
+  int lead;        // elements before the row in its first chunk
+  int vocab, lo, hi;
+  __device__ __forceinline__ Row(const Args &A, int64_t row, int rank) {
+    z = static_cast<const T *>(A.d.logits) + row * A.d.ld;
+    lead = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T));
+    vocab = (int)A.d.vocab;
+    const int all = (lead + vocab + N - 1) / N;
+    lo = rank * A.part;
+    hi = min(lo + A.part, all);
+  }
+  __device__ __forceinline__ int column(int chunk) const { return chunk * N - lead; }
+  __device__ __forceinline__ bool whole(int chunk) const { return column(chunk) >= 0 && column(chunk) + N <= vocab; }
+  __device__ __forceinline__ const uint4 *at(int chunk) const { return reinterpret_cast<const uint4 *>(z + column(chunk)); }
+  // a chunk that is not wholly the row's: its own elements, with -infinity around them
+  __device__ __forceinline__ uint4 edge(int chunk) const {
+    uint4 raw;
+    float v[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int j = column(chunk) + e;
+      v[e] = j >= 0 && j < vocab ? load_one(z + j) : -INFINITY;
+    }
+    store_vec<T, N>(reinterpret_cast<T *>(&raw), v);
+    return raw;
+  }
+};
+
+// The teacher's entries of a row, and the label as one more, in shared memory; one warp's work.
+struct Entries {
+  int32_t *col;  // column, -1: absent
+  float *zval;   // its logit
+  float *log_p;  // its log-probability
+  __device__ __forceinline__ Entries(float *base, int count)
+      : col(reinterpret_cast<int32_t *>(base)), zval(base + count), log_p(base + 2 * count) {}
+  // what entry k takes off its column's gradient, without the row's weight
+  __device__ __forceinline__ float share(const Args &A, int k, int top) const {
+    return k < top ? A.k_soft * expf(log_p[k]) : A.k_hard;
+  }
+};
+
+struct RowTerms {
+  bool soft, hard;  // whether the row has teacher's entries, a label
+};
+
+template <class T>
+__device__ __forceinline__ RowTerms load_entries(const Args &A, int64_t row, const Entries &E) {
   const dion_distill &d = A.d;
-  const int top = SOFT ? (int)d.top : 0, entries = top + (HARD ? 1 : 0);
-  uint4 *chunks = smem;  // GRAD: the block's part of the row
-  int32_t *col = reinterpret_cast<int32_t *>(smem + (GRAD ? A.part : 0));  // [entries]: column, -1: absent
-  float *share = reinterpret_cast<float *>(col + entries);                 // what the entry takes off its column's gradient
-  float *zval = share + entries;                                           // its logit
-  float *log_p = zval + entries;                                           // its teacher's log-probability
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const T *z = static_cast<const T *>(d.logits) + row * d.ld;
+  const int lane = threadIdx.x & 31, top = A.soft ? (int)d.top : 0;
+  const float inv_t = 1.f / d.temperature;
+  RowTerms r{false, false};
+  float t_max = -INFINITY;
+  bool any = false, bad = false;
+  for (int k = lane; k < top; k += 32) {
+    const int64_t id = load_index(d.ids, d.id_dtype, row * d.ld_ids + k);
+    const float t = load_any(d.teacher, d.teacher_dtype, row * d.ld_teacher + k);
+    const bool there = id >= 0 && id < d.vocab && t != -INFINITY;
+    E.col[k] = there ? (int32_t)id : -1;
+    E.log_p[k] = t;
+    E.zval[k] = there ? load_one(z + id) : 0.f;
+    any |= there;
+    bad |= there && t != t;
+    if (there) t_max = fmaxf(t_max, t);
+  }
+  if (A.hard) {
+    if (lane == 0) {
+      const int64_t y = load_index(d.labels, d.label_dtype, row);
+      const bool there = y >= 0 && y < d.vocab;
+      E.col[top] = there ? (int32_t)y : -1;
+      E.zval[top] = there ? load_one(z + y) : 0.f;
+      r.hard = there;
+    }
+    r.hard = __shfl_sync(0xffffffffu, r.hard ? 1 : 0, 0) != 0;
+  }
+  r.soft = __any_sync(0xffffffffu, any);
+  if (r.soft) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t_max = fmaxf(t_max, __shfl_xor_sync(0xffffffffu, t_max, o));
+    if (__any_sync(0xffffffffu, bad)) t_max = NAN;
+    float sum = 0.f;
+    for (int k = lane; k < top; k += 32)
+      if (E.col[k] >= 0) sum += expf((E.log_p[k] - t_max) * inv_t);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float log_sum = logf(sum);
+    for (int k = lane; k < top; k += 32) E.log_p[k] = (E.log_p[k] - t_max) * inv_t - log_sum;
+  }
+  __syncwarp();
+  return r;
+}
+
+// The row's loss; every lane has it.
+template <bool TWO>
+__device__ __forceinline__ float row_loss(const Args &A, const Entries &E, const RowTerms &r, const Stats &s) {
+  const int lane = threadIdx.x & 31, top = A.soft ? (int)A.d.top : 0;
+  const float at = anchor(s.m);
+  float loss = 0.f;
+  if (r.soft) {
+    const float log_s = logf(s.s), inv_t = 1.f / A.d.temperature;
+    for (int k = lane; k < top; k += 32) {
+      const float lp = E.log_p[k], p = expf(lp);
+      if (E.col[k] >= 0 && !(p <= 0.f)) loss += p * (lp - ((E.zval[k] - at) * inv_t - log_s));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+    loss *= A.k_soft * A.d.temperature;
+  }
+  if (r.hard) loss += A.k_hard * (logf(TWO ? s.s1 : s.s) - (E.zval[top] - at));
+  return loss;
+}
+
+// Statistics of a row from its warps' and, in a cluster, its blocks'.  Every warp merges for itself.
+template <bool TWO>
+__device__ __forceinline__ Stats block_merge(const Stats *warps, int count, float c) {
+  const int lane = threadIdx.x & 31;
+  Stats s{-INFINITY, 0.f, 0.f};
+  if (lane < count) s = warps[lane];
+  return merge_lanes<TWO>(s, c);
+}
+template <bool TWO>
+__device__ __forceinline__ Stats cluster_merge(Stats s, Stats *blocks, int count, int rank, float c) {
+  cg::cluster_group cluster = cg::this_cluster();
+  if ((int)threadIdx.x < count) *(cluster.map_shared_rank(blocks, threadIdx.x) + rank) = s;
+  cluster.sync();
+  return block_merge<TWO>(blocks, count, c);
+}
+
+// The block's barrier, also between warps at different places of the kernel.
+__device__ __forceinline__ void block_barrier() { asm volatile("barrier.sync 1, %0;" ::"r"(blockDim.x) : "memory"); }
+
+// --------------------------------------------------------------------------------- loss ---
+// One row per cluster, straight from global memory; the last warp has the teacher's entries.
+template <class T, bool TWO>
+__global__ void __launch_bounds__(kLossThreads, 3) loss_kernel(const __grid_constant__ Args A) {
+  extern __shared__ float entry_mem[];
+  __shared__ Stats warp_stats[32], block_stats[kMaxCluster];
+  const Entries E(entry_mem, (A.soft ? (int)A.d.top : 0) + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, threads = (int)blockDim.x - 32, workers = threads / 32;
   chain_enter();
   const int rank = (int)(blockIdx.x % (unsigned)A.cluster);
   const int64_t row = blockIdx.x / (unsigned)A.cluster;
-  const T *z = static_cast<const T *>(d.logits) + row * d.ld;
-  T *g = static_cast<T *>(A.grad) + (GRAD ? row * A.ldg : 0);
-  const float w = d.weights ? d.weights[row] : 1.f;
-  const int lead = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T));  // elements before the row in its first chunk
-  const int64_t all = (lead + d.vocab + N - 1) / N;                         // chunks of the row
-  const int64_t c_lo = (int64_t)rank * A.part, c_hi = c_lo + A.part < all ? c_lo + A.part : all;
-  const uint4 *zc = reinterpret_cast<const uint4 *>(z - lead);
-  // whether the gradient's rows sit at the same place within 16 bytes, so that whole chunks are stored
-  const bool same_place = GRAD && (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T)) == lead;
-
-  if (w == 0.f) {  // the same for every block of the cluster
+  const float w = A.d.weights ? A.d.weights[row] : 1.f;
+  if (w == 0.f) {  // the same for the whole cluster
     if (rank == 0 && tid == 0) A.loss[row] = 0.f;
-    if (GRAD) {
-      for (int64_t c = c_lo + tid; c < c_hi; c += kThreads) {
-        const int64_t j = c * N - lead;
-        if (same_place && j >= 0 && j + N <= d.vocab)
-          *reinterpret_cast<uint4 *>(g + j) = make_uint4(0, 0, 0, 0);
-        else
-          for (int e = 0; e < N; ++e)
-            if (j + e >= 0 && j + e < d.vocab) g[j + e] = T(0.f);
-      }
-    }
     return;
   }
-
-  // start the row's part on its way; a chunk at an end of the row that is not wholly its own is put
-  // together from single elements, with -infinity around them
-  const float inv_t = 1.f / d.temperature, ct = kLog2e * inv_t, c1 = kLog2e;
-  auto edge = [&](int64_t c, float(&v)[N]) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const int64_t j = c * N - lead + e;
-      v[e] = j >= 0 && j < d.vocab ? load_one(z + j) : -INFINITY;
-    }
-  };
-  auto whole = [&](int64_t c) { return c * N >= lead && (c + 1) * N <= lead + d.vocab; };
-  if (GRAD) {
-    for (int64_t c = c_lo + tid; c < c_hi; c += kThreads) {
-      if (whole(c)) {
-        copy_16(&chunks[c - c_lo], &zc[c]);
-      } else {
-        float v[N];
-        edge(c, v);
-        store_vec<T, N>(reinterpret_cast<T *>(&chunks[c - c_lo]), v);
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  }
-
-  // the teacher's entries, while the row is on its way: columns, logits, p
-  if (tid == 0) any = 0;
-  __syncthreads();
-  float t_max = -INFINITY;
-  if (SOFT) {
-    for (int k = tid; k < top; k += kThreads) {
-      const int64_t id = load_index(d.ids, d.id_dtype, row * d.ld_ids + k);
-      const float t = load_any(d.teacher, d.teacher_dtype, row * d.ld_teacher + k);
-      const bool there = id >= 0 && id < d.vocab && t != -INFINITY;
-      col[k] = there ? (int32_t)id : -1;
-      share[k] = t;
-      zval[k] = there ? load_one(z + id) : 0.f;
-      if (there) any = 1;
-      if (there) t_max = t > t_max || t != t ? t : t_max;  // NaN stays
-    }
-  }
-  if (HARD && tid == 0) {
-    const int64_t y = load_index(d.labels, d.label_dtype, row);
-    const bool there = y >= 0 && y < d.vocab;
-    col[top] = there ? (int32_t)y : -1;
-    share[top] = there ? w * d.hard : 0.f;
-    zval[top] = there ? load_one(z + y) : 0.f;
-  }
-  bool soft_row = false;
-  if (SOFT) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float x = __shfl_xor_sync(0xffffffffu, t_max, o);
-      t_max = x > t_max || x != x ? x : t_max;
-    }
-    if (lane == 0) red[warp] = t_max;
-    __syncthreads();
-    soft_row = any != 0;
-    for (int k = 0; k < kWarps; ++k) t_max = red[k] > t_max || red[k] != red[k] ? red[k] : t_max;
-    float sum = 0.f;
-    for (int k = tid; k < top; k += kThreads)
-      if (col[k] >= 0) sum += expf((share[k] - t_max) * inv_t);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) red2[warp] = sum;
-    __syncthreads();
-    sum = 0.f;
-    for (int k = 0; k < kWarps; ++k) sum += red2[k];
-    const float log_sum = logf(sum);
-    for (int k = tid; k < top; k += kThreads) {
-      float p = 0.f;
-      if (col[k] >= 0) {
-        log_p[k] = (share[k] - t_max) * inv_t - log_sum;
-        p = expf(log_p[k]);
-      }
-      share[k] = w * (1.f - d.hard) * d.temperature * p;
-    }
-  }
-
-  // statistics of the block's part
-  Stats s{-INFINITY, 0.f, 0.f};
-  if (GRAD) {
-    asm volatile("cp.async.wait_all;" ::: "memory");  // each thread reads only what it copied itself
-    int64_t c = c_lo + tid;
-    for (; c + 3 * kThreads < c_hi; c += 4 * kThreads) {
-      float v[4][N];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) load_vec<T, N>(reinterpret_cast<const T *>(&chunks[c - c_lo + u * kThreads]), v[u]);
-      take<T, 4, SOFT, HARD>(v, s, ct, c1);
-    }
-    for (; c < c_hi; c += kThreads) {
-      float v[1][N];
-      load_vec<T, N>(reinterpret_cast<const T *>(&chunks[c - c_lo]), v[0]);
-      take<T, 1, SOFT, HARD>(v, s, ct, c1);
-    }
+  RowTerms terms{false, false};
+  if (warp == workers) {
+    if (rank == 0) terms = load_entries<T>(A, row, E);
   } else {
-    int64_t c = c_lo + tid;
-    for (; c + 3 * kThreads < c_hi; c += 4 * kThreads) {
-      float v[4][N];
+    const Row<T> r(A, row, rank);
+    Stats s{-INFINITY, 0.f, 0.f};
+    int c = r.lo + tid;
+    for (; c + 3 * threads < r.hi; c += 4 * threads) {
+      Chunk<T> v[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t cu = c + u * kThreads;
-        if (whole(cu))
-          load_vec<T, N>(reinterpret_cast<const T *>(&zc[cu]), v[u]);
-        else
-          edge(cu, v[u]);
-      }
-      take<T, 4, SOFT, HARD>(v, s, ct, c1);
+      for (int u = 0; u < 4; ++u) v[u].raw = r.whole(c + u * threads) ? __ldcs(r.at(c + u * threads)) : r.edge(c + u * threads);
+      take<T, 4, TWO>(v, s, A.c);
     }
-    for (; c < c_hi; c += kThreads) {
-      float v[1][N];
-      if (whole(c))
-        load_vec<T, N>(reinterpret_cast<const T *>(&zc[c]), v[0]);
-      else
-        edge(c, v[0]);
-      take<T, 1, SOFT, HARD>(v, s, ct, c1);
+    for (; c < r.hi; c += threads) {
+      Chunk<T> v[1];
+      v[0].raw = r.whole(c) ? __ldcs(r.at(c)) : r.edge(c);
+      take<T, 1, TWO>(v, s, A.c);
     }
+    s = merge_lanes<TWO>(s, A.c);
+    if ((tid & 31) == 0) warp_stats[warp] = s;
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Stats x;
-    x.m = __shfl_xor_sync(0xffffffffu, s.m, o);
-    x.st = __shfl_xor_sync(0xffffffffu, s.st, o);
-    x.s1 = __shfl_xor_sync(0xffffffffu, s.s1, o);
-    s = merge<SOFT, HARD>(s, x, ct, c1);
-  }
-  if (lane == 0) warp_stats[warp] = s;
   __syncthreads();
-  if (tid == 0) {
-    for (int k = 1; k < kWarps; ++k) s = merge<SOFT, HARD>(s, warp_stats[k], ct, c1);
-    block_stats = row_stats = s;
-  }
-  if (A.cluster > 1) {
-    cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();  // every block has its statistics (and the logits of its entries)
-    if (tid == 0) {
-      Stats r = *cluster.map_shared_rank(&block_stats, 0);
-      for (int b = 1; b < A.cluster; ++b) r = merge<SOFT, HARD>(r, *cluster.map_shared_rank(&block_stats, b), ct, c1);
-      row_stats = r;
-    }
-    cluster.sync();  // the statistics were read; no block may leave before
-  } else {
-    __syncthreads();
-  }
-  s = row_stats;
-  const float at = anchor(s.m);
-
-  if (rank == 0 && warp == 0) {
-    float loss = 0.f;
-    if (SOFT && soft_row) {
-      const float log_st = logf(s.st);
-      for (int k = lane; k < top; k += 32) {
-        if (col[k] < 0) continue;
-        const float p = expf(log_p[k]);
-        if (!(p <= 0.f)) loss += p * (log_p[k] - ((zval[k] - at) * inv_t - log_st));
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-      loss *= (1.f - d.hard) * d.temperature * d.temperature;
-    }
-    if (HARD && col[top] >= 0) loss += d.hard * (logf(s.s1) - (zval[top] - at));
-    if (lane == 0) A.loss[row] = w * loss;
-  }
-  if (!GRAD) return;
-
-  // gradient without the teacher's and the label's own parts
-  const float kt = SOFT && soft_row ? w * (1.f - d.hard) * d.temperature / s.st : 0.f;
-  const float k1 = HARD && col[top] >= 0 ? w * d.hard / s.s1 : 0.f;
-  auto base = [&](float x) {
-    float r = 0.f;
-    if (SOFT) r = soft_row ? kt * exp2_fast((x - at) * ct) : 0.f;
-    if (HARD) r += col[top] >= 0 ? k1 * exp2_fast((x - at) * c1) : 0.f;
-    return r;
-  };
-  for (int64_t c = c_lo + tid; c < c_hi; c += kThreads) {
-    float v[N];
-    load_vec<T, N>(reinterpret_cast<const T *>(&chunks[c - c_lo]), v);
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = base(v[e]);
-    const int64_t j = c * N - lead;
-    if (same_place && j >= 0 && j + N <= d.vocab) {
-      store_vec<T, N>(g + j, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (j + e >= 0 && j + e < d.vocab) {
-          const float one[1] = {v[e]};
-          store_vec<T, 1>(g + j + e, one);
-        }
-    }
-  }
-  __syncthreads();  // the entries' columns are written over what was written above
-  const int64_t j_lo = c_lo * N - lead, j_hi = c_hi * N - lead;
-  for (int k = tid; k < entries; k += kThreads) {
-    const int32_t j = col[k];
-    if (j < j_lo || j >= j_hi || j < 0) continue;
-    float off = 0.f;  // of every entry with this column; the first of them writes
-    bool first = true;
-    for (int i = 0; i < entries; ++i) {
-      if (col[i] != j) continue;
-      if (i < k) first = false;
-      off += share[i];
-    }
-    if (!first) continue;
-    const float one[1] = {base(zval[k]) - off};
-    store_vec<T, 1>(g + j, one);
+  Stats s{};
+  if (A.cluster > 1 || warp == workers) s = block_merge<TWO>(warp_stats, workers, A.c);
+  if (A.cluster > 1) s = cluster_merge<TWO>(s, block_stats, A.cluster, rank, A.c);
+  if (rank == 0 && warp == workers) {
+    const float loss = row_loss<TWO>(A, E, terms, s);
+    if ((tid & 31) == 0) A.loss[row] = w * loss;
   }
 }
 
+// ---------------------------------------------------------------------- loss and gradient ---
+__device__ __forceinline__ void copy_16(uint4 *smem, const uint4 *global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(smem))),
+               "l"(global)
+               : "memory");
+}
+
+// The gradient's factors of a row: k 2^(c (z - m)) + k1 2^(log2(e) (z - m)).
+struct Factors {
+  float m, k, k1;
+};
+template <bool TWO>
+__device__ __forceinline__ Factors factors(const Args &A, const RowTerms &r, const Stats &s, float w) {
+  const float soft = r.soft ? w * A.k_soft : 0.f, hard = r.hard ? w * A.k_hard : 0.f;
+  return Factors{anchor(s.m), (TWO ? soft : soft + hard) / s.s, TWO ? hard / s.s1 : 0.f};
+}
+template <bool TWO>
+__device__ __forceinline__ float base_gradient(const Factors &f, float z, float c) {
+  float g = f.k * exp2_fast((z - f.m) * c);
+  if (TWO) g = fmaf(f.k1, exp2_fast((z - f.m) * kLog2e), g);
+  return g;
+}
+
+template <class T, bool TWO>
+__global__ void __launch_bounds__(kMaxThreads, 1) grad_kernel(const __grid_constant__ Args A) {
+  constexpr int N = 16 / sizeof(T);
+  extern __shared__ uint4 smem[];
+  __shared__ Stats warp_stats[2][32], block_stats[2][kMaxCluster];
+  __shared__ int row_terms[2];
+  const dion_distill &d = A.d;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = (int)blockDim.x - 32, workers = threads / 32;
+  const int rank = (int)(blockIdx.x % (unsigned)A.cluster), top = A.soft ? (int)d.top : 0, entries = top + (A.hard ? 1 : 0);
+  const int64_t first = blockIdx.x / (unsigned)A.cluster, stride = gridDim.x / (unsigned)A.cluster;
+  uint32_t *bitmap = reinterpret_cast<uint32_t *>(smem + (size_t)A.buffers * A.part);
+  float *entry_mem = reinterpret_cast<float *>(bitmap + A.bitmap);
+  for (int i = tid; i < A.bitmap; i += blockDim.x) bitmap[i] = 0;
+  chain_enter();
+  __syncthreads();
+  auto weight = [&](int64_t row) { return row < d.rows ? d.weights ? d.weights[row] : 1.f : 0.f; };
+
+  if (warp < workers) {
+    auto start_copy = [&](int64_t row, uint4 *to) {  // this thread's chunks of a row
+      const Row<T> r(A, row, rank);
+      for (int c = r.lo + tid; c < r.hi; c += threads) {
+        if (r.whole(c))
+          copy_16(&to[c - r.lo], r.at(c));
+        else
+          to[c - r.lo] = r.edge(c);
+      }
+    };
+    float w = weight(first), w_next = weight(first + stride);
+    if (w != 0.f) start_copy(first, smem);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    int turn = 0;
+    for (int64_t row = first; row < d.rows; row += stride, turn ^= 1) {
+      const float w_after = weight(row + 2 * stride);
+      uint4 *mine = smem + (A.buffers > 1 && turn ? A.part : 0);
+      const Row<T> r(A, row, rank);
+      T *g = static_cast<T *>(A.grad) + row * A.ldg;
+      // whole chunks are stored where the gradient's row sits at the same place within 16 bytes
+      const bool same_place = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T)) == r.lead;
+      if (A.buffers > 1) {
+        if (w_next != 0.f) start_copy(row + stride, smem + (turn ? 0 : A.part));
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+      } else {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+      }
+      Stats s{-INFINITY, 0.f, 0.f};
+      if (w != 0.f) {
+        int c = r.lo + tid;
+        for (; c + threads < r.hi; c += 2 * threads) {
+          Chunk<T> v[2];
+          v[0].raw = mine[c - r.lo], v[1].raw = mine[c - r.lo + threads];
+          take<T, 2, TWO>(v, s, A.c);
+        }
+        if (c < r.hi) {
+          Chunk<T> v[1];
+          v[0].raw = mine[c - r.lo];
+          take<T, 1, TWO>(v, s, A.c);
+        }
+        s = merge_lanes<TWO>(s, A.c);
+      }
+      if (lane == 0) warp_stats[turn][warp] = s;
+      block_barrier();
+      s = block_merge<TWO>(warp_stats[turn], workers, A.c);
+      if (A.cluster > 1) s = cluster_merge<TWO>(s, block_stats[turn], A.cluster, rank, A.c);
+      const int t = row_terms[turn];
+      const RowTerms terms{(t & 1) != 0, (t & 2) != 0};
+      const Factors f = factors<TWO>(A, terms, s, w);
+      const bool zeros = w == 0.f || t == 0;
+      const uint64_t c2 = pack2(A.c, A.c), m2 = pack2(-f.m, -f.m), k2 = pack2(f.k, f.k);
+      const uint64_t l2 = pack2(kLog2e, kLog2e), k12 = pack2(f.k1, f.k1);
+      for (int c = r.lo + tid; c < r.hi; c += threads) {
+        float v[N];
+        if (zeros) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[e] = 0.f;
+        } else {
+          Chunk<T> x;
+          x.raw = mine[c - r.lo];
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) {
+            const uint64_t z = add2(x.pair(i), m2);
+            float a, b;
+            unpack2(mul2(z, c2), a, b);
+            uint64_t y = mul2(k2, pack2(exp2_fast(a), exp2_fast(b)));
+            if (TWO) {
+              unpack2(mul2(z, l2), a, b);
+              y = fma2(k12, pack2(exp2_fast(a), exp2_fast(b)), y);
+            }
+            unpack2(y, v[2 * i], v[2 * i + 1]);
+          }
+        }
+        const int j = r.column(c);
+        if (same_place && r.whole(c)) {
+          store_vec<T, N>(g + j, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (j + e >= 0 && j + e < r.vocab) store_one(g + j + e, v[e]);
+        }
+      }
+      if (A.buffers == 1 && row + stride < d.rows) {
+        if (w_next != 0.f) start_copy(row + stride, smem);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+      w = w_next, w_next = w_after;
+    }
+    block_barrier();  // the teacher's warp writes the last row's entries
+    return;
+  }
+
+  // The teacher's warp.  A row's entries are written over what the others wrote once the next row's
+  // barrier (or the last one) shows that they are past it.
+  struct Pending {
+    int64_t row;
+    float w;
+    RowTerms terms;
+    Factors f;
+    bool twice;
+  } last{-1, 0.f, {false, false}, {}, false};
+  auto finish = [&](const Entries &E) {
+    if (last.row < 0 || last.w == 0.f) return;
+    T *g = static_cast<T *>(A.grad) + last.row * A.ldg;
+    const Row<T> r(A, last.row, rank);
+    for (int k = lane; k < entries; k += 32) {
+      const int j = E.col[k];
+      if (j < 0 || j < r.column(r.lo) || j >= r.column(r.hi)) continue;
+      float off = E.share(A, k, top);
+      if (last.twice) {  // an entry that comes several times: the first writes, with all their shares
+        bool before = false;
+        off = 0.f;
+        for (int i = 0; i < entries; ++i)
+          if (E.col[i] == j) before |= i < k, off += E.share(A, i, top);
+        if (before) continue;
+      }
+      store_one(g + j, base_gradient<TWO>(last.f, E.zval[k], A.c) - last.w * off);
+    }
+    __syncwarp();  // the entries are read; the row after next takes their place
+  };
+  int turn = 0;
+  for (int64_t row = first; row < d.rows; row += stride, turn ^= 1) {
+    const Entries E(entry_mem + turn * 3 * (top + 1), top + 1), other(entry_mem + (turn ^ 1) * 3 * (top + 1), top + 1);
+    const float w = weight(row);
+    RowTerms terms{false, false};
+    bool twice = false;
+    if (w != 0.f) {
+      terms = load_entries<T>(A, row, E);
+      // whether a column of this block's part comes twice: a bit for each, set and cleared by its entries
+      const Row<T> r(A, row, rank);
+      const int lo = r.column(r.lo), hi = r.column(r.hi);
+      for (int k = lane; k < entries; k += 32) {
+        const int j = E.col[k];
+        if (j < 0 || j < lo || j >= hi) continue;
+        const uint32_t bit = 1u << ((j - lo) & 31);
+        twice |= (atomicOr(&bitmap[(j - lo) >> 5], bit) & bit) != 0;
+      }
+      twice = __any_sync(0xffffffffu, twice);
+      for (int k = lane; k < entries; k += 32) {
+        const int j = E.col[k];
+        if (j >= 0 && j >= lo && j < hi) bitmap[(j - lo) >> 5] = 0;
+      }
+      __syncwarp();
+    }
+    if (lane == 0) row_terms[turn] = (terms.soft ? 1 : 0) | (terms.hard ? 2 : 0);
+    block_barrier();
+    Stats s = block_merge<TWO>(warp_stats[turn], workers, A.c);
+    if (A.cluster > 1) s = cluster_merge<TWO>(s, block_stats[turn], A.cluster, rank, A.c);
+    finish(other);
+    last.row = row, last.w = w, last.terms = terms, last.f = factors<TWO>(A, terms, s, w), last.twice = twice;
+    if (rank == 0) {
+      const float loss = w == 0.f ? 0.f : row_loss<TWO>(A, E, terms, s);
+      if (lane == 0) A.loss[row] = w == 0.f ? 0.f : w * loss;
+    }
+  }
+  block_barrier();
+  finish(Entries(entry_mem + (turn ^ 1) * 3 * (top + 1), top + 1));
+}
+
+// ----------------------------------------------------------------------------- dispatch ---
 dion_status check(const dion_distill *d, float *loss) {
   if (!d || d->rows < 0 || d->vocab < 1 || d->top < 0 || !is_dtype(d->dtype) || !(d->temperature > 0.f) ||
       !std::isfinite(d->temperature) || !(d->hard >= 0.f && d->hard <= 1.f))
@@ -368,34 +577,87 @@ dion_status check(const dion_distill *d, float *loss) {
   return DION_OK;
 }
 
-template <class T, bool GRAD>
-cudaError_t run(const Args &A, size_t smem, cudaStream_t s) {
-  const bool soft = A.d.hard < 1.f, hard = A.d.hard > 0.f;
-  auto kernel = soft ? hard ? distill_kernel<T, GRAD, true, true> : distill_kernel<T, GRAD, true, false>
-                     : distill_kernel<T, GRAD, false, true>;
-  const cudaError_t e = allow_dynamic_smem(kernel, smem);
-  if (e != cudaSuccess) return e;
-  return launch(kernel, A.d.rows * A.cluster, kThreads, smem, s, A.cluster, A);
+template <class... P>
+cudaError_t run(void (*kernel)(P...), const Args &A, int64_t grid, int threads, size_t smem, cudaStream_t s) {
+  if (smem > 48 * 1024 - kStaticSmem) {
+    const cudaError_t e = allow_dynamic_smem(kernel, smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch(kernel, grid, threads, smem, s, A.cluster, A);
 }
 
-dion_status enqueue(const dion_distill *d, float *loss, void *grad, int64_t ldg, bool with_grad, void *stream) {
+int num_sms() {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return DION_ERR_CUDA;
+    return 0;
+  return sms;
+}
+
+Args make_args(const dion_distill *d, float *loss) {
   Args A{};
-  A.d = *d, A.loss = loss, A.grad = grad, A.ldg = ldg;
-  const int64_t bytes = d->vocab * element_bytes(d->dtype), chunks = bytes / 16 + 2;  // the most a row can touch
-  A.cluster = 1;
-  while (A.cluster < kMaxCluster && ((with_grad && chunks * 16 > (int64_t)kPartBytes * A.cluster) ||
-                                     (d->rows * A.cluster * 2 <= sms && chunks / A.cluster > 2 * kThreads)))
-    A.cluster *= 2;
+  A.d = *d, A.loss = loss;
+  A.soft = d->hard < 1.f, A.hard = d->hard > 0.f;
+  const float t = A.soft ? d->temperature : 1.f;
+  A.c = kLog2e / t;
+  A.k_soft = (1.f - d->hard) * t, A.k_hard = d->hard;
+  return A;
+}
+// Two softmaxes only where both terms are there and differ in temperature.
+bool two_softmaxes(const Args &A) { return A.soft && A.hard && A.d.temperature != 1.f; }
+int64_t row_chunks(const dion_distill *d) { return d->vocab * element_bytes(d->dtype) / 16 + 2; }  // the most a row touches
+size_t entry_bytes(const Args &A) { return 12 * ((A.soft ? (size_t)A.d.top : 0) + 1); }
+
+dion_status enqueue_loss(const dion_distill *d, float *loss, cudaStream_t s) {
+  const int sms = num_sms();
+  if (sms == 0) return DION_ERR_CUDA;
+  Args A = make_args(d, loss);
+  const int64_t chunks = row_chunks(d);
+  A.cluster = 1;  // more blocks per row while the rows leave SMs idle and a thread has more than one round of chunks
+  while (A.cluster < kMaxCluster && d->rows * A.cluster * 2 <= sms && chunks / A.cluster > 4 * kLossThreads) A.cluster *= 2;
   A.part = (int32_t)((chunks + A.cluster - 1) / A.cluster);
-  const size_t entries = (d->hard < 1.f ? (size_t)d->top : 0) + (d->hard > 0.f ? 1 : 0);
-  const size_t smem = (with_grad ? (size_t)A.part * 16 : 0) + entries * 16;
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int threads = (int)std::min<int64_t>(kLossThreads, (A.part + 31) / 32 * 32 + 32);
+  const size_t smem = entry_bytes(A);
+  const int64_t grid = d->rows * A.cluster;
+  const bool two = two_softmaxes(A);
+  using BF = __nv_bfloat16;
   const cudaError_t e = d->dtype == DION_DTYPE_FP32
-                            ? with_grad ? run<float, true>(A, smem, s) : run<float, false>(A, smem, s)
-                            : with_grad ? run<__nv_bfloat16, true>(A, smem, s) : run<__nv_bfloat16, false>(A, smem, s);
+                            ? run(two ? loss_kernel<float, true> : loss_kernel<float, false>, A, grid, threads, smem, s)
+                            : run(two ? loss_kernel<BF, true> : loss_kernel<BF, false>, A, grid, threads, smem, s);
+  return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
+}
+
+dion_status enqueue_grad(const dion_distill *d, float *loss, void *grad, int64_t ldg, cudaStream_t s) {
+  const int sms = num_sms();
+  if (sms == 0) return DION_ERR_CUDA;
+  Args A = make_args(d, loss);
+  A.grad = grad, A.ldg = ldg;
+  const int64_t chunks = row_chunks(d);
+  const int per_chunk = 16 / element_bytes(d->dtype);
+  auto shape = [&](int cluster, int buffers) {
+    A.cluster = cluster, A.buffers = buffers;
+    A.part = (int32_t)((chunks + cluster - 1) / cluster);
+    A.bitmap = (A.part * per_chunk + 31) / 32;
+    return (size_t)A.part * 16 * buffers + 4 * (size_t)A.bitmap + 2 * entry_bytes(A);
+  };
+  const size_t most = kSmemPerSm - kSmemPerBlock - kStaticSmem;
+  int cluster = 1;
+  while (cluster < kMaxCluster && shape(cluster, 2) > most) cluster *= 2;
+  // rows that leave SMs idle are shared by more blocks, down to a chunk per thread
+  while (cluster < kMaxCluster && d->rows * cluster * 2 <= sms && chunks / cluster > kMaxThreads) cluster *= 2;
+  size_t smem = shape(cluster, 2);
+  if (smem > most) smem = shape(cluster, 1);
+  if (smem > most) return DION_ERR_UNSUPPORTED;
+  // six chunks per thread between two barriers, or one where rows are few
+  const int64_t per_thread = d->rows * cluster <= sms ? 1 : 6;
+  const int warps = (int)std::min<int64_t>(kMaxThreads / 32 - 1, std::max<int64_t>(1, (A.part / per_thread + 31) / 32));
+  const int threads = (warps + 1) * 32;
+  const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(kMaxThreads / threads, (int64_t)(kSmemPerSm / (smem + kSmemPerBlock + kStaticSmem))));
+  const int64_t clusters = std::min<int64_t>(d->rows, std::max<int64_t>(1, sms * resident / cluster));
+  const bool two = two_softmaxes(A);
+  using BF = __nv_bfloat16;
+  const cudaError_t e = d->dtype == DION_DTYPE_FP32
+                            ? run(two ? grad_kernel<float, true> : grad_kernel<float, false>, A, clusters * cluster, threads, smem, s)
+                            : run(two ? grad_kernel<BF, true> : grad_kernel<BF, false>, A, clusters * cluster, threads, smem, s);
   return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
 }
 
@@ -406,7 +668,7 @@ extern "C" {
 dion_status dion_distill_loss(const dion_distill *d, float *loss, void *stream) {
   const dion_status st = check(d, loss);
   if (st != DION_OK || d->rows == 0) return st;
-  return enqueue(d, loss, nullptr, 0, false, stream);
+  return enqueue_loss(d, loss, static_cast<cudaStream_t>(stream));
 }
 
 dion_status dion_distill_loss_grad(const dion_distill *d, float *loss, void *grad, int64_t ldg, void *stream) {
@@ -414,7 +676,7 @@ dion_status dion_distill_loss_grad(const dion_distill *d, float *loss, void *gra
   if (st != DION_OK || d->rows == 0) return st;
   if (!grad || ldg < d->vocab) return DION_ERR_INVALID_ARG;
   if (!aligned_to(grad, element_bytes(d->dtype))) return DION_ERR_ALIGNMENT;
-  return enqueue(d, loss, grad, ldg, true, stream);
+  return enqueue_grad(d, loss, grad, ldg, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -6,7 +6,8 @@
 //
 // A group of lanes holds a head as D / 2 pairs (the elements that pass are paired across their own
 // halves, with angle 0), so a rotation never leaves a lane; the mean is a shuffle sum over the group.
-// A group takes several heads of one token and computes the token's sines and cosines once.
+// A warp takes one token at a time: its sines and cosines are computed once by the warp's lanes, and
+// several heads per group are loaded before the first is used.
 #include "lm_common.cuh"
 
 #include <algorithm>
@@ -18,8 +19,12 @@ using namespace cd::lm;
 
 namespace {
 constexpr int kMaxHeadDim = 256;
+constexpr int kMaxPairs = kMaxHeadDim / 2;
+constexpr int kMaxHeads = 2048;  // of q, of k
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kForwardHeads = 4;   // heads that a group has in flight
+constexpr int kBackwardHeads = 2;
 }  // namespace
 
 struct dion_qknorm_plan {
@@ -41,10 +46,13 @@ struct Heads {
 };
 
 struct Args {
-  int64_t batch, tokens, tasks;  // tasks = batch * tokens * split
-  int32_t hq, hk, split;         // a token's heads are dealt to `split` groups
-  int32_t dim, half;             // half = rotary / 2
-  int32_t chunks, group;         // chunks of V pairs per head, lanes per head
+  int64_t batch, tokens;  // sequences, tokens of each
+  int64_t tasks;          // forward: tokens of all sequences * parts
+  int32_t hq, hk;
+  int32_t q_batches, batches;  // batches of heads (one kind each) of q, of q and k
+  int32_t parts;               // warps that share a token's batches
+  int32_t dim, half;           // half = rotary / 2
+  int32_t group;               // lanes per head
   float eps;
   const void *pos;
   int64_t pos_sb;
@@ -55,6 +63,30 @@ struct Args {
   float *dwq, *dwk;
   float *partial;
   uint32_t *finished;
+};
+
+// V elements as they sit in memory.
+template <class T, int V>
+struct Raw {
+  static constexpr int kBytes = V * (int)sizeof(T);
+  uint32_t w[kBytes >= 4 ? kBytes / 4 : 1];
+  __device__ __forceinline__ void load(const T *p) {
+    if constexpr (kBytes == 16) {
+      const uint4 x = *reinterpret_cast<const uint4 *>(p);
+      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else if constexpr (kBytes == 8) {
+      const uint2 x = *reinterpret_cast<const uint2 *>(p);
+      w[0] = x.x, w[1] = x.y;
+    } else if constexpr (kBytes == 4) {
+      w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t *>(p);
+    }
+  }
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
 };
 
 // Where pair u of a head sits: its first element, and the distance to the second.  Pairs at and beyond
@@ -70,29 +102,40 @@ __device__ __forceinline__ void pair_place(int u, int dim, int half, int &at, in
   }
 }
 
-// A lane's V pairs (a, b) of one chunk; V divides half and dim / 2 - half unless interleaved.
-template <class T, int V, bool INTER>
-__device__ __forceinline__ void load_pairs(const T *x, int u, int dim, int half, float (&a)[V], float (&b)[V]) {
-  int at, apart;
-  pair_place<INTER>(u, dim, half, at, apart);
-  if (INTER) {
-    float lo[V], hi[V];
-    load_vec<T, V>(x + at, lo);
-    load_vec<T, V>(x + at + V, hi);
+// A lane's pairs of a head: NC chunks of V, `group` lanes apart; V divides half and dim / 2 - half unless
+// interleaved, when a chunk's pairs are 2 V neighbouring elements.
+template <class T, int V, int NC, bool INTER>
+struct HeadPairs {
+  Raw<T, V> lo[NC], hi[NC];
+  __device__ __forceinline__ void load(const T *x, bool on, int in_group, const Args &A) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      a[e] = 2 * e < V ? lo[(2 * e) % V] : hi[(2 * e) % V];
-      b[e] = 2 * e + 1 < V ? lo[(2 * e + 1) % V] : hi[(2 * e + 1) % V];
+    for (int n = 0; n < NC; ++n) {
+      const int u = (in_group + n * A.group) * V;
+#pragma unroll
+      for (uint32_t &w : lo[n].w) w = 0;
+#pragma unroll
+      for (uint32_t &w : hi[n].w) w = 0;
+      if (on && 2 * u < A.dim) {
+        int at, apart;
+        pair_place<INTER>(u, A.dim, A.half, at, apart);
+        lo[n].load(x + at);
+        hi[n].load(x + at + (INTER ? V : apart));
+      }
     }
-  } else {
-    load_vec<T, V>(x + at, a);
-    load_vec<T, V>(x + at + apart, b);
   }
-}
+  __device__ __forceinline__ float a(int n, int e) const {
+    if (!INTER) return lo[n].at(e);
+    return 2 * e < V ? lo[n].at((2 * e) % V) : hi[n].at((2 * e) % V);
+  }
+  __device__ __forceinline__ float b(int n, int e) const {
+    if (!INTER) return hi[n].at(e);
+    return 2 * e + 1 < V ? lo[n].at((2 * e + 1) % V) : hi[n].at((2 * e + 1) % V);
+  }
+};
 template <class T, int V, bool INTER>
-__device__ __forceinline__ void store_pairs(T *x, int u, int dim, int half, const float (&a)[V], const float (&b)[V]) {
+__device__ __forceinline__ void store_pairs(T *x, int u, const Args &A, const float (&a)[V], const float (&b)[V]) {
   int at, apart;
-  pair_place<INTER>(u, dim, half, at, apart);
+  pair_place<INTER>(u, A.dim, A.half, at, apart);
   if (INTER) {
     float lo[V], hi[V];
 #pragma unroll
@@ -114,197 +157,222 @@ __device__ __forceinline__ float group_sum(float v, int group) {
   return v;
 }
 
-// cos and sin of a token's angle for pair u.  position * turn wraps modulo one turn exactly; the top 32
-// bits, as a signed fraction of half a turn, are within 2^-32 of it, and fp32's rounding of that is
-// 2^-25 of half a turn at most.
-__device__ __forceinline__ void pair_angle(const Args &A, int64_t position, int u, float &c, float &s) {
-  c = 1.f, s = 0.f;
-  if (u < A.half) {
-    const int32_t part = (int32_t)(((uint64_t)position * A.turn[u]) >> 32);
-    sincospif((float)part * 0x1p-31f, &s, &c);
+// Sines and cosines of a token's pairs into the warp's shared memory.  position * turn wraps modulo one
+// turn exactly; the top 32 bits, as a signed fraction of half a turn, are within 2^-31 of it, and
+// fp32's rounding of that is 2^-25 of half a turn at most.
+__device__ __forceinline__ void token_angles(const Args &A, int64_t position, float *cs, float *sn) {
+  __syncwarp();  // the last token's were read
+  for (int u = threadIdx.x & 31; u < A.dim / 2; u += 32) {
+    float c = 1.f, s = 0.f;
+    if (u < A.half) {
+      const int32_t part = (int32_t)(((uint64_t)position * A.turn[u]) >> 32);
+      sincospif((float)part * 0x1p-31f, &s, &c);
+    }
+    cs[u] = c, sn[u] = s;
+  }
+  __syncwarp();
+}
+
+// The weights of both kinds by pairs, in shared memory: [kind][first or second of the pair][pair].
+template <bool INTER>
+__device__ __forceinline__ void stage_weights(const Args &A, float (&w)[2][2][kMaxPairs]) {
+  for (int i = threadIdx.x; i < 2 * A.dim; i += kThreads) {
+    const int kind = i / A.dim, r = i - kind * A.dim, second = r >= A.dim / 2, u = r - second * (A.dim / 2);
+    int at, apart;
+    pair_place<INTER>(u, A.dim, A.half, at, apart);
+    const float *from = kind ? A.wk : A.wq;
+    w[kind][second][u] = from ? from[at + second * apart] : 1.f;
+  }
+  __syncthreads();
+}
+
+// V neighbouring floats of shared memory for each of a lane's chunks.
+template <int V, int NC>
+__device__ __forceinline__ void read_pairs(const float *from, int in_group, const Args &A, float (&v)[NC][V]) {
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const int u = (in_group + n * A.group) * V;
+    load_vec<float, V>(from + (2 * u < A.dim ? u : 0), v[n]);
   }
 }
 
-// What a group works on: a token and its first head; heads h, h + split, ... of q, then of k.
-struct Task {
+struct Token {
   int64_t b, t;
-  int32_t head;
-  int64_t position;
+  __device__ __forceinline__ Token(const Args &A, int64_t i) {
+    if (i <= 0x7fffffff && A.tokens <= 0x7fffffff) {  // a 64-bit division costs more than a head
+      b = (uint32_t)i / (uint32_t)A.tokens;
+    } else {
+      b = i / A.tokens;
+    }
+    t = i - b * A.tokens;
+  }
+  __device__ __forceinline__ int64_t position(const Args &A) const {
+    return A.pos ? load_index(A.pos, A.pos_dtype, b * A.pos_sb + t) : t;
+  }
+  template <class T>
+  __device__ __forceinline__ T *heads(const Heads &H) const {
+    return static_cast<T *>(H.p) + b * H.sb + t * H.st;
+  }
 };
-__device__ __forceinline__ Task task_of(const Args &A, int64_t i) {
-  Task k;
-  const int64_t token = i / A.split;
-  k.head = (int32_t)(i - token * A.split);
-  k.b = token / A.tokens;
-  k.t = token - k.b * A.tokens;
-  k.position = A.pos ? load_index(A.pos, A.pos_dtype, k.b * A.pos_sb + k.t) : k.t;
-  return k;
-}
-template <class T>
-__device__ __forceinline__ T *head_of(const Heads &H, const Task &k, int h) {
-  return static_cast<T *>(H.p) + k.b * H.sb + k.t * H.st + h * H.sh;
-}
 
 // ------------------------------------------------------------------------------ forward ---
-// NC chunks of V pairs per lane, `group` lanes apart.
 template <class T, int V, int NC, bool INTER>
-__global__ void __launch_bounds__(kThreads) forward_kernel(const Args A) {
+__global__ void __launch_bounds__(kThreads) forward_kernel(const __grid_constant__ Args A) {
+  constexpr int U = kForwardHeads;
+  __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs];
   chain_enter();
-  const int lane = threadIdx.x & 31, in_group = lane & (A.group - 1);
-  const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / A.group;
-  const bool live = i < A.tasks;  // the shuffles need every lane
-  const Task k = task_of(A, live ? i : 0);
-  float c[NC][V], s[NC][V];
-#pragma unroll
-  for (int n = 0; n < NC; ++n)
-#pragma unroll
-    for (int e = 0; e < V; ++e) pair_angle(A, k.position, (in_group + n * A.group) * V + e, c[n][e], s[n][e]);
+  stage_weights<INTER>(A, w);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_group = lane & (A.group - 1), groups = 32 / A.group;
+  const int64_t task = (int64_t)blockIdx.x * kWarps + warp;
+  if (task >= A.tasks) return;
+  const int64_t i = task <= 0x7fffffff ? (int64_t)((uint32_t)task / (uint32_t)A.parts) : task / A.parts;
+  const Token tok(A, i);
+  const int64_t position = tok.position(A);
   const float inv_dim = 1.f / (float)A.dim;
-  const int heads = A.hq + A.hk;
-  for (int h0 = 0; h0 < heads; h0 += A.split) {  // the same count for every group
-    const int h = h0 + k.head;
-    const bool on = live && h < heads, is_q = h < A.hq;
-    const T *x = head_of<const T>(is_q ? A.q : A.k, k, is_q ? h : h - A.hq);
-    float a[NC][V], b[NC][V], sum = 0.f;
+  bool angles_ready = false;
+  for (int batch = (int)(task - i * A.parts); batch < A.batches; batch += A.parts) {
+    const int kind = batch >= A.q_batches;
+    const int heads = kind ? A.hk : A.hq, h0 = (batch - (kind ? A.q_batches : 0)) * U * groups + lane / A.group;
+    const Heads &X = kind ? A.k : A.q, &Y = kind ? A.ok : A.oq;
+    const T *x = tok.heads<const T>(X);
+    T *y = tok.heads<T>(Y);
+    HeadPairs<T, V, NC, INTER> p[U];
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      const int u = (in_group + n * A.group) * V;
-      if (on && 2 * u < A.dim) {
-        load_pairs<T, V, INTER>(x, u, A.dim, A.half, a[n], b[n]);
+    for (int k = 0; k < U; ++k) p[k].load(x + (h0 + k * groups) * X.sh, h0 + k * groups < heads, in_group, A);
+    if (!angles_ready) token_angles(A, position, angles[warp][0], angles[warp][1]);
+    angles_ready = true;
+    float c[NC][V], s[NC][V], wa[NC][V], wb[NC][V];
+    read_pairs<V, NC>(angles[warp][0], in_group, A, c);
+    read_pairs<V, NC>(angles[warp][1], in_group, A, s);
+    read_pairs<V, NC>(w[kind][0], in_group, A, wa);
+    read_pairs<V, NC>(w[kind][1], in_group, A, wb);
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum = fmaf(a[n][e], a[n][e], fmaf(b[n][e], b[n][e], sum));
-      }
-    }
-    const float r = rsqrtf(group_sum(sum, A.group) * inv_dim + A.eps);
-    if (!on) continue;
-    const float *w = is_q ? A.wq : A.wk;
-    T *y = head_of<T>(is_q ? A.oq : A.ok, k, is_q ? h : h - A.hq);
+    for (int k = 0; k < U; ++k) {
+      if ((batch - (kind ? A.q_batches : 0)) * U * groups + k * groups >= heads) break;  // the same for the whole warp
+      float sum = 0.f;
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      const int u = (in_group + n * A.group) * V;
-      if (2 * u >= A.dim) continue;
-      float wa[V], wb[V];
+      for (int n = 0; n < NC; ++n)
 #pragma unroll
-      for (int e = 0; e < V; ++e) wa[e] = wb[e] = 1.f;
-      if (w)
+        for (int e = 0; e < V; ++e) sum = fmaf(p[k].a(n, e), p[k].a(n, e), fmaf(p[k].b(n, e), p[k].b(n, e), sum));
+      const float r = rsqrtf(group_sum(sum, A.group) * inv_dim + A.eps);
+      const int h = h0 + k * groups;
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        const int u = (in_group + n * A.group) * V;
+        if (h >= heads || 2 * u >= A.dim) continue;
+        float a[V], b[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          int at, apart;
-          pair_place<INTER>(u + e, A.dim, A.half, at, apart);
-          wa[e] = w[at], wb[e] = w[at + apart];
+          const float ua = p[k].a(n, e) * r * wa[n][e], ub = p[k].b(n, e) * r * wb[n][e];
+          a[e] = ua * c[n][e] - ub * s[n][e];
+          b[e] = ub * c[n][e] + ua * s[n][e];
         }
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float ua = a[n][e] * r * wa[e], ub = b[n][e] * r * wb[e];
-        a[n][e] = ua * c[n][e] - ub * s[n][e];
-        b[n][e] = ub * c[n][e] + ua * s[n][e];
+        store_pairs<T, V, INTER>(y + h * Y.sh, u, A, a, b);
       }
-      store_pairs<T, V, INTER>(y, u, A.dim, A.half, a[n], b[n]);
     }
   }
 }
 
 // ----------------------------------------------------------------------------- backward ---
+// A warp keeps to one batch of heads and goes over tokens, so that its sums of dw stay in registers.
 template <class T, int V, int NC, bool INTER>
-__global__ void __launch_bounds__(kThreads) backward_kernel(const Args A) {
-  __shared__ float red[kWarps][2 * kMaxHeadDim];
+__global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Args A) {
+  constexpr int U = kBackwardHeads;
+  __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs], red[kWarps][2 * kMaxHeadDim];
   __shared__ bool last;
   chain_enter();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_group = lane & (A.group - 1);
-  const int64_t per_block = kThreads / A.group, stride = per_block * gridDim.x;
-  const int64_t first = (int64_t)blockIdx.x * per_block + threadIdx.x / A.group;
-  const int64_t rounds = (A.tasks + stride - 1) / stride;
+  stage_weights<INTER>(A, w);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_group = lane & (A.group - 1), groups = 32 / A.group;
+  const int64_t all = A.batch * A.tokens;
+  const int unit = blockIdx.x * kWarps + warp, batch = unit % A.batches;
+  const int64_t first = unit / A.batches, stride = ((int64_t)gridDim.x * kWarps - batch + A.batches - 1) / A.batches;
+  const int kind = batch >= A.q_batches;
+  const int heads = kind ? A.hk : A.hq, h_first = (batch - (kind ? A.q_batches : 0)) * U * groups, h0 = h_first + lane / A.group;
+  const Heads &X = kind ? A.k : A.q, &G = kind ? A.gk : A.gq, &Y = kind ? A.ok : A.oq;
   const float inv_dim = 1.f / (float)A.dim;
-  const int heads = A.hq + A.hk;
-  float dqa[NC][V], dqb[NC][V], dka[NC][V], dkb[NC][V];  // this lane's sums of dwq, dwk
+  float wa[NC][V], wb[NC][V], da[NC][V], db[NC][V];  // weights, and this lane's sums of their gradients
+  read_pairs<V, NC>(w[kind][0], in_group, A, wa);
+  read_pairs<V, NC>(w[kind][1], in_group, A, wb);
 #pragma unroll
   for (int n = 0; n < NC; ++n)
 #pragma unroll
-    for (int e = 0; e < V; ++e) dqa[n][e] = dqb[n][e] = dka[n][e] = dkb[n][e] = 0.f;
-  for (int64_t round = 0; round < rounds; ++round) {
-    const int64_t i = first + round * stride;
-    const bool live = i < A.tasks;
-    const Task k = task_of(A, live ? i : 0);
+    for (int e = 0; e < V; ++e) da[n][e] = db[n][e] = 0.f;
+  for (int64_t i = first; i < all; i += stride) {
+    const Token tok(A, i);
+    const T *x = tok.heads<const T>(X), *g = tok.heads<const T>(G);
+    T *y = tok.heads<T>(Y);
+    HeadPairs<T, V, NC, INTER> p[U], q[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const bool on = h0 + k * groups < heads;
+      p[k].load(x + (h0 + k * groups) * X.sh, on, in_group, A);
+      q[k].load(g + (h0 + k * groups) * G.sh, on, in_group, A);
+    }
+    token_angles(A, tok.position(A), angles[warp][0], angles[warp][1]);
     float c[NC][V], s[NC][V];
+    read_pairs<V, NC>(angles[warp][0], in_group, A, c);
+    read_pairs<V, NC>(angles[warp][1], in_group, A, s);
 #pragma unroll
-    for (int n = 0; n < NC; ++n)
+    for (int k = 0; k < U; ++k) {
+      if (h_first + k * groups >= heads) break;  // the same for the whole warp
+      float ga[NC][V], gb[NC][V], sum = 0.f, dot = 0.f;
 #pragma unroll
-      for (int e = 0; e < V; ++e) pair_angle(A, k.position, (in_group + n * A.group) * V + e, c[n][e], s[n][e]);
-    for (int h0 = 0; h0 < heads; h0 += A.split) {
-      const int h = h0 + k.head;
-      const bool on = live && h < heads, is_q = h < A.hq;
-      const int hh = is_q ? h : h - A.hq;
-      const T *x = head_of<const T>(is_q ? A.q : A.k, k, hh);
-      const T *g = head_of<const T>(is_q ? A.gq : A.gk, k, hh);
-      const float *w = is_q ? A.wq : A.wk;
-      float a[NC][V], b[NC][V], ga[NC][V], gb[NC][V], sum = 0.f, dot = 0.f;
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const int u = (in_group + n * A.group) * V;
-        if (on && 2 * u < A.dim) {
-          load_pairs<T, V, INTER>(x, u, A.dim, A.half, a[n], b[n]);
-          load_pairs<T, V, INTER>(g, u, A.dim, A.half, ga[n], gb[n]);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            int at, apart;
-            pair_place<INTER>(u + e, A.dim, A.half, at, apart);
-            const float wa = w ? w[at] : 1.f, wb = w ? w[at + apart] : 1.f;
-            const float ra = ga[n][e] * c[n][e] + gb[n][e] * s[n][e], rb = gb[n][e] * c[n][e] - ga[n][e] * s[n][e];
-            ga[n][e] = ra, gb[n][e] = rb;
-            sum = fmaf(a[n][e], a[n][e], fmaf(b[n][e], b[n][e], sum));
-            dot = fmaf(ra * wa, a[n][e], fmaf(rb * wb, b[n][e], dot));
-          }
-        }
-      }
-      const float r = rsqrtf(group_sum(sum, A.group) * inv_dim + A.eps);
-      dot = group_sum(dot, A.group) * inv_dim * r * r;  // n mean(w gu n) = x r * r * mean(w gu x)
-      if (!on) continue;
-      T *y = head_of<T>(is_q ? A.oq : A.ok, k, hh);
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const int u = (in_group + n * A.group) * V;
-        if (2 * u >= A.dim) continue;
+      for (int n = 0; n < NC; ++n)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          int at, apart;
-          pair_place<INTER>(u + e, A.dim, A.half, at, apart);
-          const float wa = w ? w[at] : 1.f, wb = w ? w[at + apart] : 1.f;
-          const float da = ga[n][e] * a[n][e] * r, db = gb[n][e] * b[n][e] * r;
-          if (is_q)
-            dqa[n][e] += da, dqb[n][e] += db;
-          else
-            dka[n][e] += da, dkb[n][e] += db;
-          a[n][e] = r * (wa * ga[n][e] - a[n][e] * dot);
-          b[n][e] = r * (wb * gb[n][e] - b[n][e] * dot);
+          const float a = p[k].a(n, e), b = p[k].b(n, e), oa = q[k].a(n, e), ob = q[k].b(n, e);
+          ga[n][e] = oa * c[n][e] + ob * s[n][e];
+          gb[n][e] = ob * c[n][e] - oa * s[n][e];
+          sum = fmaf(a, a, fmaf(b, b, sum));
+          dot = fmaf(ga[n][e] * wa[n][e], a, fmaf(gb[n][e] * wb[n][e], b, dot));
         }
-        store_pairs<T, V, INTER>(y, u, A.dim, A.half, a[n], b[n]);
+      sum = group_sum(sum, A.group);
+      dot = group_sum(dot, A.group);
+      const float r = rsqrtf(sum * inv_dim + A.eps);
+      const float back = dot * inv_dim * r * r * r;  // dx = r w gu - x r^3 mean(w gu x)
+      const int h = h0 + k * groups;
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        const int u = (in_group + n * A.group) * V;
+        if (h >= heads || 2 * u >= A.dim) continue;
+        float oa[V], ob[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float a = p[k].a(n, e), b = p[k].b(n, e), ra = r * ga[n][e], rb = r * gb[n][e];
+          da[n][e] = fmaf(ra, a, da[n][e]), db[n][e] = fmaf(rb, b, db[n][e]);
+          oa[e] = ra * wa[n][e] - a * back;
+          ob[e] = rb * wb[n][e] - b * back;
+        }
+        store_pairs<T, V, INTER>(y + h * Y.sh, u, A, oa, ob);
       }
     }
   }
   if (!A.dwq && !A.dwk) return;
   // the block's sums of dw: over the groups of a warp, then over the warps, then over the blocks, each
   // in a fixed order; the last block to finish adds up the blocks
+  for (int d = lane; d < 2 * A.dim; d += 32) red[warp][d] = 0.f;
+  __syncwarp();
 #pragma unroll
   for (int n = 0; n < NC; ++n)
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      float v[4] = {dqa[n][e], dqb[n][e], dka[n][e], dkb[n][e]};
-#pragma unroll
-      for (int m = 0; m < 4; ++m)
-        for (int o = A.group; o < 32; o <<= 1) v[m] += __shfl_xor_sync(0xffffffffu, v[m], o);
+      float va = da[n][e], vb = db[n][e];
+      for (int o = A.group; o < 32; o <<= 1) {
+        va += __shfl_xor_sync(0xffffffffu, va, o);
+        vb += __shfl_xor_sync(0xffffffffu, vb, o);
+      }
       const int u = (in_group + n * A.group) * V + e;
       if (lane < A.group && 2 * u < A.dim) {
         int at, apart;
         pair_place<INTER>(u, A.dim, A.half, at, apart);
-        red[warp][at] = v[0], red[warp][at + apart] = v[1];
-        red[warp][A.dim + at] = v[2], red[warp][A.dim + at + apart] = v[3];
+        red[warp][kind * A.dim + at] = va, red[warp][kind * A.dim + at + apart] = vb;
       }
     }
   __syncthreads();
   for (int d = threadIdx.x; d < 2 * A.dim; d += kThreads) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) v += red[w][d];
+    for (int k = 0; k < kWarps; ++k) v += red[k][d];
     A.partial[(int64_t)blockIdx.x * 2 * A.dim + d] = v;
   }
   __threadfence();
@@ -352,6 +420,7 @@ dion_status check_shape(const dion_qknorm_plan *p, const dion_qk_shape *s) {
       !is_dtype(s->dtype))
     return DION_ERR_INVALID_ARG;
   if (s->positions && !is_index(s->position_dtype)) return DION_ERR_INVALID_ARG;
+  if (s->heads > kMaxHeads || s->kv_heads > kMaxHeads) return DION_ERR_UNSUPPORTED;
   if (s->positions && !aligned_to(s->positions, s->position_dtype == DION_INDEX_INT64 ? 8 : 4)) return DION_ERR_ALIGNMENT;
   const int64_t limit = (int64_t)1 << 40, per = ((int64_t)s->heads + s->kv_heads) * p->head_dim;
   if (s->batch > 0 && s->tokens > 0 && (per > limit || s->batch > limit / per || s->tokens > limit / per / s->batch))
@@ -359,27 +428,18 @@ dion_status check_shape(const dion_qknorm_plan *p, const dion_qk_shape *s) {
   return DION_OK;
 }
 
-Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int v, int nc) {
+Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int v, int nc, int heads_in_flight) {
   Args A{};
   A.batch = s->batch, A.tokens = s->tokens, A.hq = s->heads, A.hk = s->kv_heads;
   A.dim = p->head_dim, A.half = p->rotary / 2, A.eps = p->eps;
   A.pos = s->positions, A.pos_sb = s->position_batch_stride, A.pos_dtype = s->position_dtype;
   A.turn = p->turn, A.partial = p->partial, A.finished = p->finished;
-  A.chunks = p->head_dim / 2 / v;
   A.group = 1;
-  while (A.group * nc < A.chunks) A.group *= 2;
+  while (A.group * nc * v < p->head_dim / 2) A.group *= 2;
+  const int per = heads_in_flight * (32 / A.group);
+  A.q_batches = (int32_t)(((int64_t)A.hq + per - 1) / per);
+  A.batches = A.q_batches + (int32_t)(((int64_t)A.hk + per - 1) / per);
   return A;
-}
-
-// Heads per group: enough groups to fill the GPU first, then up to 8 heads of a token for each group,
-// which share its sines and cosines.
-void split_heads(Args &A, int num_sms) {
-  const int heads = A.hq + A.hk;
-  const int64_t tokens = A.batch * A.tokens, want = (int64_t)num_sms * 1024 / A.group;
-  int64_t split = (heads + 7) / 8;
-  if (tokens * split < want) split = std::min<int64_t>(heads, (want + tokens - 1) / tokens);
-  A.split = (int32_t)split;
-  A.tasks = tokens * split;
 }
 
 template <class T, bool INTER, class F>
@@ -423,7 +483,8 @@ dion_status dion_qknorm_plan_create(int32_t head_dim, int32_t rotary_dim, int32_
   p->head_dim = head_dim, p->rotary = rotary_dim, p->interleaved = interleaved != 0, p->eps = eps;
   cudaError_t e = cudaGetDevice(&p->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->num_sms, cudaDevAttrMultiProcessorCount, p->device);
-  p->max_blocks = 2 * (int64_t)p->num_sms;
+  // two resident blocks per SM, and a warp for every batch of the most heads that a call may have
+  p->max_blocks = std::max<int64_t>(2 * (int64_t)p->num_sms, 2 * kMaxHeads / kBackwardHeads / kWarps);
   const size_t o_partial = sizeof(turn), o_done = o_partial + sizeof(float) * 2 * head_dim * p->max_blocks;
   if (e == cudaSuccess) e = cudaMalloc(&p->ws, o_done + 16);
   if (e == cudaSuccess) {
@@ -462,10 +523,13 @@ dion_status dion_qknorm_forward(dion_qknorm_plan *p, const dion_qk_shape *s, con
   const Heads h[4] = {heads_of(s->heads ? q : nullptr), heads_of(s->kv_heads ? k : nullptr),
                       heads_of(s->heads ? q_out : nullptr), heads_of(s->kv_heads ? k_out : nullptr)};
   const int v = pair_width(p, s, h, 4);
-  Args A = make_args(p, s, v, chunks_per_lane(v));
+  Args A = make_args(p, s, v, chunks_per_lane(v), kForwardHeads);
   A.q = h[0], A.k = h[1], A.oq = h[2], A.ok = h[3], A.wq = wq, A.wk = wk;
-  split_heads(A, p->num_sms);
-  const int64_t blocks = (A.tasks * A.group + kThreads - 1) / kThreads;
+  // a warp per token, or more where the tokens do not give every SM its 16 warps
+  const int64_t all = s->batch * s->tokens;
+  A.parts = (int32_t)std::min<int64_t>(A.batches, ((int64_t)p->num_sms * 16 + all - 1) / all);
+  A.tasks = all * A.parts;
+  const int64_t blocks = (A.tasks + kWarps - 1) / kWarps;
   if (blocks > INT32_MAX) return DION_ERR_UNSUPPORTED;
   const cudaError_t e = with_kernel(s->dtype, v, p->interleaved, [&](auto t, auto V, auto NC, auto I) {
     return launch(forward_kernel<decltype(t), decltype(V)::value, decltype(NC)::value, decltype(I)::value>, blocks, kThreads,
@@ -497,11 +561,12 @@ dion_status dion_qknorm_backward(dion_qknorm_plan *p, const dion_qk_shape *s, co
     h[i] = heads_of(n ? in[i] : nullptr);
   }
   const int v = pair_width(p, s, h, 6);
-  Args A = make_args(p, s, v, chunks_per_lane(v));
+  Args A = make_args(p, s, v, chunks_per_lane(v), kBackwardHeads);
   A.gq = h[0], A.gk = h[1], A.q = h[2], A.k = h[3], A.oq = h[4], A.ok = h[5];
   A.wq = wq, A.wk = wk, A.dwq = dwq, A.dwk = dwk;
-  split_heads(A, p->num_sms);
-  const int64_t blocks = std::min(p->max_blocks, (A.tasks * A.group + kThreads - 1) / kThreads);
+  const int64_t units = s->batch * s->tokens * A.batches;
+  const int64_t blocks = std::max<int64_t>(std::min(p->max_blocks, (units + kWarps - 1) / kWarps),
+                                           (A.batches + kWarps - 1) / kWarps);  // a warp for every batch of heads
   const cudaError_t e = with_kernel(s->dtype, v, p->interleaved, [&](auto t, auto V, auto NC, auto I) {
     return launch(backward_kernel<decltype(t), decltype(V)::value, decltype(NC)::value, decltype(I)::value>, blocks, kThreads,
                   0, cs, 1, A);

@@ -107,11 +107,20 @@ class DionError(RuntimeError):
 
 
 _lib = None
+# The operators' entry points once more, with structs taken as packed bytes (see lm.py).
+_packed = None
+
+
+def _packed_entry_points(lib):
+    P, I64 = C.c_void_p, C.c_int64
+    sig = {"dion_qknorm_forward": (P,) * 9, "dion_qknorm_backward": (P,) * 13, "dion_distill_loss": (P,) * 3,
+           "dion_distill_loss_grad": (P, P, P, I64, P)}
+    return {name: C.CFUNCTYPE(C.c_int, *args)((name, lib)) for name, args in sig.items()}
 
 
 def load(path: str = LIB_PATH) -> C.CDLL:
     """Loads libcurvadion.so (built by paper_2512_13728_gb300.build) and declares its signatures."""
-    global _lib
+    global _lib, _packed
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
@@ -184,6 +193,7 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     if lib.dion_abi_version() != DION_ABI_VERSION:  # the structs above follow this version's header
         raise ImportError(f"{path} has ABI version {lib.dion_abi_version()}, this binding expects {DION_ABI_VERSION}: "
                           "rebuild it with `python -m paper_2512_13728_gb300.build --force`")
+    _packed = _packed_entry_points(lib)
     _lib = lib
     return lib
 
@@ -346,8 +356,8 @@ def dion_embed_plan_create(vocab: int, dim: int, max_tokens: int) -> int:
 def dion_embed_lookup(plan: int, tokens: int, token_dtype: int, num_tokens: int, table: int, table_dtype: int, ldt: int,
                       scale: float, out: int, out_dtype: int, ldo: int, stream: int) -> None:
     """All pointers are device addresses (ints)."""
-    st = load().dion_embed_lookup(plan, tokens, token_dtype, num_tokens, table, table_dtype, ldt, scale, out, out_dtype,
-                                  ldo, stream)
+    st = _lib.dion_embed_lookup(plan, tokens, token_dtype, num_tokens, table, table_dtype, ldt, scale, out, out_dtype, ldo,
+                                stream)
     if st != DION_OK:
         raise DionError(st, "dion_embed_lookup")
 
@@ -356,8 +366,8 @@ def dion_embed_gradient(plan: int, tokens: int, token_dtype: int, num_tokens: in
                         scale: float, table_grad: int, table_grad_dtype: int, ldd: int, accumulate: int,
                         stream: int) -> None:
     """All pointers are device addresses (ints)."""
-    st = load().dion_embed_gradient(plan, tokens, token_dtype, num_tokens, grad, grad_dtype, ldg, scale, table_grad,
-                                    table_grad_dtype, ldd, accumulate, stream)
+    st = _lib.dion_embed_gradient(plan, tokens, token_dtype, num_tokens, grad, grad_dtype, ldg, scale, table_grad,
+                                  table_grad_dtype, ldd, accumulate, stream)
     if st != DION_OK:
         raise DionError(st, "dion_embed_gradient")
 
@@ -377,16 +387,17 @@ def dion_qknorm_plan_create(head_dim: int, rotary_dim: int, interleaved: bool, t
     return out.value
 
 
-def dion_qknorm_forward(plan: int, shape: dion_qk_shape, q, k, wq, wk, q_out, k_out, stream: int) -> None:
-    """q, k, q_out, k_out: dion_heads (k, k_out may be None); wq, wk: device addresses or None."""
-    st = load().dion_qknorm_forward(plan, shape, q, k, wq, wk, q_out, k_out, stream)
+def dion_qknorm_forward(plan: int, shape: bytes, q, k, wq, wk, q_out, k_out, stream: int) -> None:
+    """shape: a packed dion_qk_shape; q, k, q_out, k_out: packed dion_heads (those of k may be None); wq, wk:
+    device addresses or None."""
+    st = _packed["dion_qknorm_forward"](plan, shape, q, k, wq, wk, q_out, k_out, stream)
     if st != DION_OK:
         raise DionError(st, "dion_qknorm_forward")
 
 
-def dion_qknorm_backward(plan: int, shape: dion_qk_shape, gq, gk, q, k, wq, wk, dq, dk, dwq, dwk, stream: int) -> None:
-    """gq, gk, q, k, dq, dk: dion_heads (those of k may be None); the others: device addresses or None."""
-    st = load().dion_qknorm_backward(plan, shape, gq, gk, q, k, wq, wk, dq, dk, dwq, dwk, stream)
+def dion_qknorm_backward(plan: int, shape: bytes, gq, gk, q, k, wq, wk, dq, dk, dwq, dwk, stream: int) -> None:
+    """As dion_qknorm_forward; dwq, dwk: device addresses or None."""
+    st = _packed["dion_qknorm_backward"](plan, shape, gq, gk, q, k, wq, wk, dq, dk, dwq, dwk, stream)
     if st != DION_OK:
         raise DionError(st, "dion_qknorm_backward")
 
@@ -396,13 +407,16 @@ def dion_qknorm_plan_destroy(plan: int) -> None:
         load().dion_qknorm_plan_destroy(plan)
 
 
-def dion_distill_loss(args: dion_distill, loss: int, stream: int) -> None:
-    st = load().dion_distill_loss(args, loss, stream)
+def dion_distill_loss(args: bytes, loss: int, stream: int) -> None:
+    """args: a packed dion_distill."""
+    load()
+    st = _packed["dion_distill_loss"](args, loss, stream)
     if st != DION_OK:
         raise DionError(st, "dion_distill_loss")
 
 
-def dion_distill_loss_grad(args: dion_distill, loss: int, grad: int, ldg: int, stream: int) -> None:
-    st = load().dion_distill_loss_grad(args, loss, grad, ldg, stream)
+def dion_distill_loss_grad(args: bytes, loss: int, grad: int, ldg: int, stream: int) -> None:
+    load()
+    st = _packed["dion_distill_loss_grad"](args, loss, grad, ldg, stream)
     if st != DION_OK:
         raise DionError(st, "dion_distill_loss_grad")

@@ -267,3 +267,31 @@ def test_c_refusals(cd):
     assert lib.dion_distill_loss_grad(args(), p, None, 100, None) == 1
     assert lib.dion_distill_loss_grad(args(), p, p, 99, None) == 1
     assert lib.dion_distill_loss_grad(args(), p, C.c_void_p(0x9002), 100, None) == 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("v", [500, 70000])
+def test_rows_of_the_lowest_value(cd, dtype, v):
+    """A mask of the type's lowest value over a whole row leaves a uniform softmax, at every temperature."""
+    z = torch.full((2, v), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+    z[1] = torch.finfo(dtype).max
+    ids, t = torch.tensor([[3, 5]] * 2, device="cuda"), torch.zeros(2, 2, device="cuda")
+    labels = torch.full((2,), 7, device="cuda")
+    for T, hard in ((1.0, 0.0), (0.25, 0.5), (4.0, 0.5)):
+        l, g = cd.distill_loss_grad(z, ids, t, T, labels, hard)
+        want = (1 - hard) * T * T * math.log(v / 2) + hard * math.log(v)
+        assert ((l.double() - want).abs() <= (v / 128 + 64) * u * want).all()
+        rest = ((1 - hard) * T + hard) / v
+        assert ((g[:, 8:].double() - rest).abs() <= rest * (OUT[dtype] + (v / 128 + 64) * u)).all()
+
+
+def test_packed_structs_follow_the_header():
+    from paper_2512_13728_gb300 import lm, native
+
+    for packed, struct in ((lm._DISTILL, native.dion_distill), (lm._HEADS, native.dion_heads),
+                           (lm._QK_SHAPE, native.dion_qk_shape)):
+        assert packed.size == C.sizeof(struct)
+        values = list(range(1, 1 + len(struct._fields_)))
+        got = struct.from_buffer_copy(packed.pack(*values))
+        assert [getattr(got, f[0]) for f in struct._fields_] == values
