@@ -11,21 +11,22 @@
 // row costs one block barrier, between the sums and the gradient.  One warp of the block does all that
 // belongs to the teacher's entries, a row ahead of the others.
 #include "lm_common.cuh"
+#include "tc_common.cuh"
 
 #include <algorithm>
 #include <cmath>
-#include <cooperative_groups.h>
 
 using namespace cd;
 using namespace cd::lm;
-namespace cg = cooperative_groups;
 
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMaxThreads = 1024;
+constexpr int kMaxWorkers = 20, kMaxTeachers = 4;  // warps of the gradient's blocks
+constexpr int kGradThreads = 32 * (kMaxWorkers + kMaxTeachers);
 constexpr int kLossThreads = 512;
 constexpr int kMaxCluster = 8;
+constexpr int kBatch = 4;  // of the teacher's entries that a lane loads together
 constexpr size_t kSmemPerSm = 227 * 1024, kSmemPerBlock = 1024;  // of an SM; what the system takes of each block's
 constexpr int kStaticSmem = 2048;                                // at most, of the kernels here
 
@@ -37,13 +38,14 @@ struct Args {
   int32_t cluster, part;  // blocks per row, chunks of 16 bytes per block
   int32_t buffers;        // rows in shared memory: 2, or 1 where two do not fit
   int32_t bitmap;         // words
-  float c;                // log2(e) / temperature of the first softmax
+  int32_t teachers;       // warps for the teacher's entries
+  float c, inv_t;         // log2(e) / temperature of the first softmax, 1 / temperature
   float k_soft, k_hard;   // (1 - hard) T, hard
   int32_t soft, hard;     // which terms the loss has
 };
 
 // Running maximum, sum at the loss's temperature, and where there are two softmaxes the sum at 1.
-struct Stats {
+struct __align__(16) Stats {
   float m, s, s1;
 };
 
@@ -79,24 +81,20 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 // What is subtracted in the exponent: the maximum, or 0 for a set without finite logits.
 __device__ __forceinline__ float anchor(float m) { return m == -INFINITY ? 0.f : m; }
 
-template <bool TWO>
-__device__ __forceinline__ Stats merge(const Stats &a, const Stats &b, float c) {
-  Stats r;
-  r.m = fmaxf(a.m, b.m);
-  const float da = a.m - anchor(r.m), db = b.m - anchor(r.m);
-  r.s = a.s * exp2_fast(da * c) + b.s * exp2_fast(db * c);
-  r.s1 = TWO ? a.s1 * exp2_fast(da * kLog2e) + b.s1 * exp2_fast(db * kLog2e) : 0.f;
-  return r;
-}
+// The same over a warp's lanes, in every lane: the maximum first, then one correction per lane.
 template <bool TWO>
 __device__ __forceinline__ Stats merge_lanes(Stats s, float c) {
+  float m = s.m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float d = s.m - anchor(m);
+  s.m = m;
+  s.s *= exp2_fast(d * c);
+  if (TWO) s.s1 *= exp2_fast(d * kLog2e);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    Stats x;
-    x.m = __shfl_xor_sync(0xffffffffu, s.m, o);
-    x.s = __shfl_xor_sync(0xffffffffu, s.s, o);
-    x.s1 = TWO ? __shfl_xor_sync(0xffffffffu, s.s1, o) : 0.f;
-    s = merge<TWO>(s, x, c);
+    s.s += __shfl_xor_sync(0xffffffffu, s.s, o);
+    if (TWO) s.s1 += __shfl_xor_sync(0xffffffffu, s.s1, o);
   }
   return s;
 }
@@ -175,24 +173,28 @@ __device__ __forceinline__ float load_any(const void *p, int32_t dtype, int64_t 
 }
 
 // One row as a block sees it: chunks of 16 bytes at multiples of 16, of which the block's are [lo, hi).
+// The first and the last chunk of a row may be only partly its own (edges); thread t of the block's
+// `threads` has chunks lo + t, lo + t + threads, ...
 template <class T>
 struct Row {
   static constexpr int N = 16 / sizeof(T);
   const T *z;
-  int lead;        // elements before the row in its first chunk
+  int lead;  // elements before the row in its first chunk
   int vocab, lo, hi;
+  int whole_hi;     // end of the block's chunks before a last edge
+  bool first_edge;  // chunk lo is an edge at the row's beginning
   __device__ __forceinline__ Row(const Args &A, int64_t row, int rank) {
     z = static_cast<const T *>(A.d.logits) + row * A.d.ld;
     lead = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T));
     vocab = (int)A.d.vocab;
-    const int all = (lead + vocab + N - 1) / N;
     lo = rank * A.part;
-    hi = min(lo + A.part, all);
+    hi = min(lo + A.part, (lead + vocab + N - 1) / N);
+    whole_hi = min(hi, (lead + vocab) / N);
+    first_edge = lead > 0 && rank == 0;
   }
   __device__ __forceinline__ int column(int chunk) const { return chunk * N - lead; }
-  __device__ __forceinline__ bool whole(int chunk) const { return column(chunk) >= 0 && column(chunk) + N <= vocab; }
   __device__ __forceinline__ const uint4 *at(int chunk) const { return reinterpret_cast<const uint4 *>(z + column(chunk)); }
-  // a chunk that is not wholly the row's: its own elements, with -infinity around them
+  // an edge's own elements, with -infinity around them
   __device__ __forceinline__ uint4 edge(int chunk) const {
     uint4 raw;
     float v[N];
@@ -215,7 +217,7 @@ struct Entries {
       : col(reinterpret_cast<int32_t *>(base)), zval(base + count), log_p(base + 2 * count) {}
   // what entry k takes off its column's gradient, without the row's weight
   __device__ __forceinline__ float share(const Args &A, int k, int top) const {
-    return k < top ? A.k_soft * expf(log_p[k]) : A.k_hard;
+    return k < top ? A.k_soft * exp2_fast(log_p[k] * kLog2e) : A.k_hard;
   }
 };
 
@@ -223,51 +225,91 @@ struct RowTerms {
   bool soft, hard;  // whether the row has teacher's entries, a label
 };
 
-template <class T>
-__device__ __forceinline__ RowTerms load_entries(const Args &A, int64_t row, const Entries &E) {
+// A lane's entries of one batch: loads that nothing waits for until they are used.
+struct Batch {
+  int32_t id[kBatch];  // -1: absent
+  float t[kBatch];
+};
+__device__ __forceinline__ Batch fetch_entries(const Args &A, int64_t row, int k0) {
   const dion_distill &d = A.d;
-  const T *z = static_cast<const T *>(d.logits) + row * d.ld;
-  const int lane = threadIdx.x & 31, top = A.soft ? (int)d.top : 0;
-  const float inv_t = 1.f / d.temperature;
-  RowTerms r{false, false};
+  const int top = A.soft ? (int)d.top : 0;
+  Batch b;
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) {
+    const int k = k0 + u * 32 + (threadIdx.x & 31);
+    b.id[u] = -1, b.t[u] = -INFINITY;
+    if (k < top) {
+      const int64_t i = load_index(d.ids, d.id_dtype, row * d.ld_ids + k);
+      b.t[u] = load_any(d.teacher, d.teacher_dtype, row * d.ld_teacher + k);
+      b.id[u] = i >= 0 && i < d.vocab ? (int32_t)i : -1;
+    }
+  }
+  return b;
+}
+template <class T>
+__device__ __forceinline__ void gather_logits(const Args &A, int64_t row, Batch &b, float (&z)[kBatch]) {
+  const T *from = static_cast<const T *>(A.d.logits) + row * A.d.ld;
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) {
+    if (b.t[u] == -INFINITY) b.id[u] = -1;
+    z[u] = b.id[u] >= 0 ? load_one(from + b.id[u]) : 0.f;
+  }
+}
+
+// Entries of a row into shared memory, with the teacher's softmax.  The first batch and its logits are
+// given; the label's column is `label` (-1: absent), its logit `label_z`.
+template <class T>
+__device__ __forceinline__ RowTerms set_entries(const Args &A, int64_t row, const Entries &E, Batch b, float (&z)[kBatch],
+                                                int32_t label, float label_z) {
+  const int lane = threadIdx.x & 31, top = A.soft ? (int)A.d.top : 0;
   float t_max = -INFINITY;
   bool any = false, bad = false;
-  for (int k = lane; k < top; k += 32) {
-    const int64_t id = load_index(d.ids, d.id_dtype, row * d.ld_ids + k);
-    const float t = load_any(d.teacher, d.teacher_dtype, row * d.ld_teacher + k);
-    const bool there = id >= 0 && id < d.vocab && t != -INFINITY;
-    E.col[k] = there ? (int32_t)id : -1;
-    E.log_p[k] = t;
-    E.zval[k] = there ? load_one(z + id) : 0.f;
-    any |= there;
-    bad |= there && t != t;
-    if (there) t_max = fmaxf(t_max, t);
-  }
-  if (A.hard) {
-    if (lane == 0) {
-      const int64_t y = load_index(d.labels, d.label_dtype, row);
-      const bool there = y >= 0 && y < d.vocab;
-      E.col[top] = there ? (int32_t)y : -1;
-      E.zval[top] = there ? load_one(z + y) : 0.f;
-      r.hard = there;
+  for (int k0 = 0; k0 < top; k0 += 32 * kBatch) {
+    if (k0 > 0) {
+      b = fetch_entries(A, row, k0);
+      gather_logits<T>(A, row, b, z);
     }
-    r.hard = __shfl_sync(0xffffffffu, r.hard ? 1 : 0, 0) != 0;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int k = k0 + u * 32 + lane;
+      if (k >= top) break;
+      E.col[k] = b.id[u];
+      E.log_p[k] = b.t[u];
+      E.zval[k] = z[u];
+      if (b.id[u] < 0) continue;
+      any = true;
+      bad |= b.t[u] != b.t[u];
+      t_max = fmaxf(t_max, b.t[u]);
+    }
   }
-  r.soft = __any_sync(0xffffffffu, any);
+  if (A.hard && lane == 0) E.col[top] = label, E.zval[top] = label_z;
+  const RowTerms r{__any_sync(0xffffffffu, any) != 0, A.hard && label >= 0};
   if (r.soft) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t_max = fmaxf(t_max, __shfl_xor_sync(0xffffffffu, t_max, o));
     if (__any_sync(0xffffffffu, bad)) t_max = NAN;
     float sum = 0.f;
-    for (int k = lane; k < top; k += 32)
-      if (E.col[k] >= 0) sum += expf((E.log_p[k] - t_max) * inv_t);
+#pragma unroll 4
+    for (int k = lane; k < top; k += 32) sum += E.col[k] >= 0 ? exp2_fast((E.log_p[k] - t_max) * A.c) : 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float log_sum = logf(sum);
-    for (int k = lane; k < top; k += 32) E.log_p[k] = (E.log_p[k] - t_max) * inv_t - log_sum;
+#pragma unroll 4
+    for (int k = lane; k < top; k += 32) E.log_p[k] = (E.log_p[k] - t_max) * A.inv_t - log_sum;
   }
   __syncwarp();
   return r;
+}
+
+// A row's label and its logit, in every lane.
+__device__ __forceinline__ int32_t fetch_label(const Args &A, int64_t row) {
+  if (!A.hard) return -1;
+  const int64_t y = load_index(A.d.labels, A.d.label_dtype, row);
+  return y >= 0 && y < A.d.vocab ? (int32_t)y : -1;
+}
+template <class T>
+__device__ __forceinline__ float label_logit(const Args &A, int64_t row, int32_t label) {
+  return label >= 0 ? load_one(static_cast<const T *>(A.d.logits) + row * A.d.ld + label) : 0.f;
 }
 
 // The row's loss; every lane has it.
@@ -277,10 +319,12 @@ __device__ __forceinline__ float row_loss(const Args &A, const Entries &E, const
   const float at = anchor(s.m);
   float loss = 0.f;
   if (r.soft) {
-    const float log_s = logf(s.s), inv_t = 1.f / A.d.temperature;
+    const float log_s = logf(s.s);
+#pragma unroll 4
     for (int k = lane; k < top; k += 32) {
-      const float lp = E.log_p[k], p = expf(lp);
-      if (E.col[k] >= 0 && !(p <= 0.f)) loss += p * (lp - ((E.zval[k] - at) * inv_t - log_s));
+      const float lp = E.log_p[k], p = exp2_fast(lp * kLog2e);
+      const float part = p * (lp - ((E.zval[k] - at) * A.inv_t - log_s));
+      loss += E.col[k] >= 0 && !(p <= 0.f) ? part : 0.f;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
@@ -298,17 +342,19 @@ __device__ __forceinline__ Stats block_merge(const Stats *warps, int count, floa
   if (lane < count) s = warps[lane];
   return merge_lanes<TWO>(s, c);
 }
-template <bool TWO>
-__device__ __forceinline__ Stats cluster_merge(Stats s, Stats *blocks, int count, int rank, float c) {
-  cg::cluster_group cluster = cg::this_cluster();
-  if ((int)threadIdx.x < count) *(cluster.map_shared_rank(blocks, threadIdx.x) + rank) = s;
-  cluster.sync();
-  return block_merge<TWO>(blocks, count, c);
+// Writes a block's statistics into its place of block `to`'s array and, with a barrier, counts their
+// bytes on that block's barrier of the same place (no fence: a release at cluster scope would wait for the
+// gradient's stores).
+__device__ __forceinline__ void send(const Stats &s, Stats *blocks, int to, int rank, uint64_t *bar) {
+  const uint32_t at = tc::cluster_addr(blocks + rank, (uint32_t)to);
+  if (bar)
+    asm volatile(
+        "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(at),
+        "f"(s.m), "f"(s.s), "f"(s.s1), "f"(0.f), "r"(tc::cluster_addr(bar, (uint32_t)to))
+        : "memory");
+  else
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(s.m), "f"(s.s), "f"(s.s1), "f"(0.f) : "memory");
 }
-
-// The block's barrier, also between warps at different places of the kernel.
-__device__ __forceinline__ void block_barrier() { asm volatile("barrier.sync 1, %0;" ::"r"(blockDim.x) : "memory"); }
-
 // --------------------------------------------------------------------------------- loss ---
 // One row per cluster, straight from global memory; the last warp has the teacher's entries.
 template <class T, bool TWO>
@@ -327,21 +373,37 @@ __global__ void __launch_bounds__(kLossThreads, 3) loss_kernel(const __grid_cons
   }
   RowTerms terms{false, false};
   if (warp == workers) {
-    if (rank == 0) terms = load_entries<T>(A, row, E);
+    if (rank == 0) {
+      Batch b = fetch_entries(A, row, 0);
+      const int32_t label = fetch_label(A, row);
+      float z[kBatch];
+      gather_logits<T>(A, row, b, z);
+      terms = set_entries<T>(A, row, E, b, z, label, label_logit<T>(A, row, label));
+    }
   } else {
     const Row<T> r(A, row, rank);
     Stats s{-INFINITY, 0.f, 0.f};
     int c = r.lo + tid;
-    for (; c + 3 * threads < r.hi; c += 4 * threads) {
+    Chunk<T> one[1];
+    if (tid == 0 && r.first_edge) {
+      one[0].raw = r.edge(c);
+      take<T, 1, TWO>(one, s, A.c);
+      c += threads;
+    }
+    const uint4 *from = r.at(c);
+    for (; c + 3 * threads < r.whole_hi; c += 4 * threads, from += 4 * threads) {
       Chunk<T> v[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u].raw = r.whole(c + u * threads) ? __ldcs(r.at(c + u * threads)) : r.edge(c + u * threads);
+      for (int u = 0; u < 4; ++u) v[u].raw = __ldcs(from + u * threads);
       take<T, 4, TWO>(v, s, A.c);
     }
-    for (; c < r.hi; c += threads) {
-      Chunk<T> v[1];
-      v[0].raw = r.whole(c) ? __ldcs(r.at(c)) : r.edge(c);
-      take<T, 1, TWO>(v, s, A.c);
+    for (; c < r.whole_hi; c += threads, from += threads) {
+      one[0].raw = __ldcs(from);
+      take<T, 1, TWO>(one, s, A.c);
+    }
+    if (c < r.hi) {
+      one[0].raw = r.edge(c);
+      take<T, 1, TWO>(one, s, A.c);
     }
     s = merge_lanes<TWO>(s, A.c);
     if ((tid & 31) == 0) warp_stats[warp] = s;
@@ -349,7 +411,11 @@ __global__ void __launch_bounds__(kLossThreads, 3) loss_kernel(const __grid_cons
   __syncthreads();
   Stats s{};
   if (A.cluster > 1 || warp == workers) s = block_merge<TWO>(warp_stats, workers, A.c);
-  if (A.cluster > 1) s = cluster_merge<TWO>(s, block_stats, A.cluster, rank, A.c);
+  if (A.cluster > 1) {
+    if (tid == 0) send(s, block_stats, 0, rank, nullptr);
+    tc::cluster_sync();
+    if (rank == 0) s = block_merge<TWO>(block_stats, A.cluster, A.c);
+  }
   if (rank == 0 && warp == workers) {
     const float loss = row_loss<TWO>(A, E, terms, s);
     if ((tid & 31) == 0) A.loss[row] = w * loss;
@@ -357,12 +423,6 @@ __global__ void __launch_bounds__(kLossThreads, 3) loss_kernel(const __grid_cons
 }
 
 // ---------------------------------------------------------------------- loss and gradient ---
-__device__ __forceinline__ void copy_16(uint4 *smem, const uint4 *global) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(smem))),
-               "l"(global)
-               : "memory");
-}
-
 // The gradient's factors of a row: k 2^(c (z - m)) + k1 2^(log2(e) (z - m)).
 struct Factors {
   float m, k, k1;
@@ -379,46 +439,93 @@ __device__ __forceinline__ float base_gradient(const Factors &f, float z, float 
   return g;
 }
 
+// Bounded wait for the statistics of every block of the cluster.
+__device__ __forceinline__ bool wait_stats(uint64_t *bar, uint32_t parity) {
+  const uint64_t t0 = tc::globaltimer_ns();
+  for (uint32_t i = 1;; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, "
+        "p;\n}\n"
+        : "=r"(ok)
+        : "r"(tc::smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((i & 255u) == 0 && tc::globaltimer_ns() - t0 > tc::kWaitLimitNs) return false;
+  }
+}
+
+// A block's warps are workers (the first ones), which copy, sum and write rows, and teachers.  Row n of a
+// block belongs to teacher n % teachers.  Named barrier 1 + n % 4 is row n's: all workers, that teacher
+// (which brings the row's entries and takes its statistics) and the teacher of row n - 1 (which now
+// writes that row's entries over what the workers wrote there).  So a teacher has `teachers` - 1 rows of
+// time for its loads and softmax, and a worker meets one barrier per row.
 template <class T, bool TWO>
-__global__ void __launch_bounds__(kMaxThreads, 1) grad_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_constant__ Args A) {
   constexpr int N = 16 / sizeof(T);
   extern __shared__ uint4 smem[];
   __shared__ Stats warp_stats[2][32], block_stats[2][kMaxCluster];
-  __shared__ int row_terms[2];
+  __shared__ uint64_t arrived[2];  // bytes of block_stats
+  __shared__ int row_terms[4];
   const dion_distill &d = A.d;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = (int)blockDim.x - 32, workers = threads / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, teachers = A.teachers;
+  const int workers = (int)blockDim.x / 32 - teachers, threads = workers * 32;
   const int rank = (int)(blockIdx.x % (unsigned)A.cluster), top = A.soft ? (int)d.top : 0, entries = top + (A.hard ? 1 : 0);
   const int64_t first = blockIdx.x / (unsigned)A.cluster, stride = gridDim.x / (unsigned)A.cluster;
+  const int rows = (int)((d.rows - first + stride - 1) / stride);  // of this block
   uint32_t *bitmap = reinterpret_cast<uint32_t *>(smem + (size_t)A.buffers * A.part);
   float *entry_mem = reinterpret_cast<float *>(bitmap + A.bitmap);
   for (int i = tid; i < A.bitmap; i += blockDim.x) bitmap[i] = 0;
+  if (A.cluster > 1) {
+    if (tid == 0) {
+      tc::mbar_init(&arrived[0], 1);
+      tc::mbar_init(&arrived[1], 1);
+      tc::fence_mbar_init();
+    }
+    tc::cluster_sync();
+  } else {
+    __syncthreads();
+  }
   chain_enter();
-  __syncthreads();
   auto weight = [&](int64_t row) { return row < d.rows ? d.weights ? d.weights[row] : 1.f : 0.f; };
+  auto barrier = [&](int n) { asm volatile("barrier.sync %0, %1;" ::"r"(1 + (n & 3)), "r"(threads + 64) : "memory"); };
+  // row n's statistics, after its barrier
+  auto statistics = [&](int n) {
+    Stats s = block_merge<TWO>(warp_stats[n & 1], workers, A.c);
+    if (A.cluster > 1) {
+      uint64_t *bar = &arrived[n & 1];
+      if (tid == 0) tc::mbar_expect_tx(bar, (uint32_t)(A.cluster * sizeof(Stats)));
+      if (tid < A.cluster) send(s, block_stats[n & 1], tid, rank, bar);
+      const bool ok = wait_stats(bar, (uint32_t)(n >> 1) & 1);
+      s = block_merge<TWO>(block_stats[n & 1], A.cluster, A.c);
+      if (!ok) s.s = s.s1 = NAN;  // a row whose statistics never came
+    }
+    return s;
+  };
 
   if (warp < workers) {
-    auto start_copy = [&](int64_t row, uint4 *to) {  // this thread's chunks of a row
-      const Row<T> r(A, row, rank);
-      for (int c = r.lo + tid; c < r.hi; c += threads) {
-        if (r.whole(c))
-          copy_16(&to[c - r.lo], r.at(c));
-        else
-          to[c - r.lo] = r.edge(c);
-      }
+    auto start_copy = [&](const Row<T> &r, uint4 *to) {  // this thread's chunks of a row
+      int c = r.lo + tid;
+      to += tid;
+      if (tid == 0 && r.first_edge) *to = r.edge(c), c += threads, to += threads;
+      const uint4 *from = r.at(c);
+#pragma unroll 4
+      for (; c < r.whole_hi; c += threads, from += threads, to += threads)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to)), "l"(from) : "memory");
+      if (c < r.hi) *to = r.edge(c);
     };
     float w = weight(first), w_next = weight(first + stride);
-    if (w != 0.f) start_copy(first, smem);
+    Row<T> r(A, first, rank);
+    if (w != 0.f) start_copy(r, smem);
     asm volatile("cp.async.commit_group;" ::: "memory");
-    int turn = 0;
-    for (int64_t row = first; row < d.rows; row += stride, turn ^= 1) {
+    for (int n = 0; n < rows; ++n) {
+      const int64_t row = first + n * stride;
       const float w_after = weight(row + 2 * stride);
-      uint4 *mine = smem + (A.buffers > 1 && turn ? A.part : 0);
-      const Row<T> r(A, row, rank);
+      const uint4 *mine = smem + (A.buffers > 1 && (n & 1) ? A.part : 0) + tid;
+      const Row<T> r_next(A, row + stride, rank);
       T *g = static_cast<T *>(A.grad) + row * A.ldg;
-      // whole chunks are stored where the gradient's row sits at the same place within 16 bytes
-      const bool same_place = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T)) == r.lead;
       if (A.buffers > 1) {
-        if (w_next != 0.f) start_copy(row + stride, smem + (turn ? 0 : A.part));
+        if (w_next != 0.f) start_copy(r_next, smem + (n & 1 ? 0 : A.part));
         asm volatile("cp.async.commit_group;" ::: "memory");
         asm volatile("cp.async.wait_group 1;" ::: "memory");
       } else {
@@ -426,134 +533,148 @@ __global__ void __launch_bounds__(kMaxThreads, 1) grad_kernel(const __grid_const
       }
       Stats s{-INFINITY, 0.f, 0.f};
       if (w != 0.f) {
-        int c = r.lo + tid;
-        for (; c + threads < r.hi; c += 2 * threads) {
-          Chunk<T> v[2];
-          v[0].raw = mine[c - r.lo], v[1].raw = mine[c - r.lo + threads];
-          take<T, 2, TWO>(v, s, A.c);
+        int left = r.hi - r.lo - tid;
+        const uint4 *from = mine;
+        for (; left > 3 * threads; left -= 4 * threads, from += 4 * threads) {
+          Chunk<T> v[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[u].raw = from[u * threads];
+          take<T, 4, TWO>(v, s, A.c);
         }
-        if (c < r.hi) {
+        for (; left > 0; left -= threads, from += threads) {
           Chunk<T> v[1];
-          v[0].raw = mine[c - r.lo];
+          v[0].raw = from[0];
           take<T, 1, TWO>(v, s, A.c);
         }
         s = merge_lanes<TWO>(s, A.c);
       }
-      if (lane == 0) warp_stats[turn][warp] = s;
-      block_barrier();
-      s = block_merge<TWO>(warp_stats[turn], workers, A.c);
-      if (A.cluster > 1) s = cluster_merge<TWO>(s, block_stats[turn], A.cluster, rank, A.c);
-      const int t = row_terms[turn];
-      const RowTerms terms{(t & 1) != 0, (t & 2) != 0};
-      const Factors f = factors<TWO>(A, terms, s, w);
+      if (lane == 0) warp_stats[n & 1][warp] = s;
+      barrier(n);
+      s = statistics(n);
+      const int t = row_terms[n & 3];
+      const Factors f = factors<TWO>(A, RowTerms{(t & 1) != 0, (t & 2) != 0}, s, w);
       const bool zeros = w == 0.f || t == 0;
+      // whole chunks are stored where the gradient's row sits at the same place within 16 bytes
+      const bool same_place = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T)) == r.lead;
       const uint64_t c2 = pack2(A.c, A.c), m2 = pack2(-f.m, -f.m), k2 = pack2(f.k, f.k);
       const uint64_t l2 = pack2(kLog2e, kLog2e), k12 = pack2(f.k1, f.k1);
-      for (int c = r.lo + tid; c < r.hi; c += threads) {
+      auto gradient = [&](const uint4 &raw, float(&v)[N]) {
+        Chunk<T> x;
+        x.raw = raw;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          const uint64_t z = add2(x.pair(i), m2);
+          float a, b;
+          unpack2(mul2(z, c2), a, b);
+          uint64_t y = mul2(k2, pack2(exp2_fast(a), exp2_fast(b)));
+          if (TWO) {
+            unpack2(mul2(z, l2), a, b);
+            y = fma2(k12, pack2(exp2_fast(a), exp2_fast(b)), y);
+          }
+          unpack2(y, v[2 * i], v[2 * i + 1]);
+        }
+      };
+      auto single = [&](int c, const uint4 &raw) {  // element by element
         float v[N];
+        gradient(raw, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const int j = r.column(c) + e;
+          if (j >= 0 && j < r.vocab) store_one(g + j, zeros ? 0.f : v[e]);
+        }
+      };
+      int c = r.lo + tid;
+      const uint4 *from = mine;
+      if (tid == 0 && r.first_edge) single(c, *from), c += threads, from += threads;
+      if (same_place) {
+        uint4 *to = reinterpret_cast<uint4 *>(g + r.column(c));
         if (zeros) {
-#pragma unroll
-          for (int e = 0; e < N; ++e) v[e] = 0.f;
+          for (; c < r.whole_hi; c += threads, from += threads, to += threads) *to = make_uint4(0, 0, 0, 0);
         } else {
-          Chunk<T> x;
-          x.raw = mine[c - r.lo];
-#pragma unroll
-          for (int i = 0; i < N / 2; ++i) {
-            const uint64_t z = add2(x.pair(i), m2);
-            float a, b;
-            unpack2(mul2(z, c2), a, b);
-            uint64_t y = mul2(k2, pack2(exp2_fast(a), exp2_fast(b)));
-            if (TWO) {
-              unpack2(mul2(z, l2), a, b);
-              y = fma2(k12, pack2(exp2_fast(a), exp2_fast(b)), y);
-            }
-            unpack2(y, v[2 * i], v[2 * i + 1]);
+#pragma unroll 2
+          for (; c < r.whole_hi; c += threads, from += threads, to += threads) {
+            float v[N];
+            gradient(*from, v);
+            store_vec<T, N>(reinterpret_cast<T *>(to), v);
           }
         }
-        const int j = r.column(c);
-        if (same_place && r.whole(c)) {
-          store_vec<T, N>(g + j, v);
-        } else {
-#pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (j + e >= 0 && j + e < r.vocab) store_one(g + j + e, v[e]);
-        }
       }
-      if (A.buffers == 1 && row + stride < d.rows) {
-        if (w_next != 0.f) start_copy(row + stride, smem);
+      for (; c < r.hi; c += threads, from += threads) single(c, *from);
+      if (A.buffers == 1 && n + 1 < rows) {
+        if (w_next != 0.f) start_copy(r_next, smem);
         asm volatile("cp.async.commit_group;" ::: "memory");
       }
       w = w_next, w_next = w_after;
+      r = r_next;
     }
-    block_barrier();  // the teacher's warp writes the last row's entries
-    return;
-  }
-
-  // The teacher's warp.  A row's entries are written over what the others wrote once the next row's
-  // barrier (or the last one) shows that they are past it.
-  struct Pending {
-    int64_t row;
-    float w;
-    RowTerms terms;
-    Factors f;
-    bool twice;
-  } last{-1, 0.f, {false, false}, {}, false};
-  auto finish = [&](const Entries &E) {
-    if (last.row < 0 || last.w == 0.f) return;
-    T *g = static_cast<T *>(A.grad) + last.row * A.ldg;
-    const Row<T> r(A, last.row, rank);
-    for (int k = lane; k < entries; k += 32) {
-      const int j = E.col[k];
-      if (j < 0 || j < r.column(r.lo) || j >= r.column(r.hi)) continue;
-      float off = E.share(A, k, top);
-      if (last.twice) {  // an entry that comes several times: the first writes, with all their shares
-        bool before = false;
-        off = 0.f;
-        for (int i = 0; i < entries; ++i)
-          if (E.col[i] == j) before |= i < k, off += E.share(A, i, top);
-        if (before) continue;
+    barrier(rows);  // the last row's teacher writes its entries
+  } else {
+    const int teacher = warp - workers;
+    const Entries E(entry_mem + teacher * 3 * (top + 1), top + 1);
+    if (teacher == teachers - 1) barrier(0);  // no row came before
+    for (int n = teacher; n <= rows; n += teachers) {
+      const int64_t row = first + n * stride;
+      const float w = weight(row);
+      if (n == rows) {
+        barrier(n);
+        break;
       }
-      store_one(g + j, base_gradient<TWO>(last.f, E.zval[k], A.c) - last.w * off);
-    }
-    __syncwarp();  // the entries are read; the row after next takes their place
-  };
-  int turn = 0;
-  for (int64_t row = first; row < d.rows; row += stride, turn ^= 1) {
-    const Entries E(entry_mem + turn * 3 * (top + 1), top + 1), other(entry_mem + (turn ^ 1) * 3 * (top + 1), top + 1);
-    const float w = weight(row);
-    RowTerms terms{false, false};
-    bool twice = false;
-    if (w != 0.f) {
-      terms = load_entries<T>(A, row, E);
-      // whether a column of this block's part comes twice: a bit for each, set and cleared by its entries
+      RowTerms terms{false, false};
+      if (w != 0.f) {
+        Batch b = fetch_entries(A, row, 0);
+        const int32_t label = fetch_label(A, row);
+        float z[kBatch];
+        gather_logits<T>(A, row, b, z);
+        terms = set_entries<T>(A, row, E, b, z, label, label_logit<T>(A, row, label));
+      }
+      if (lane == 0) row_terms[n & 3] = (terms.soft ? 1 : 0) | (terms.hard ? 2 : 0);
+      barrier(n);
+      const Stats s = statistics(n);
       const Row<T> r(A, row, rank);
       const int lo = r.column(r.lo), hi = r.column(r.hi);
-      for (int k = lane; k < entries; k += 32) {
-        const int j = E.col[k];
-        if (j < 0 || j < lo || j >= hi) continue;
-        const uint32_t bit = 1u << ((j - lo) & 31);
-        twice |= (atomicOr(&bitmap[(j - lo) >> 5], bit) & bit) != 0;
+      bool twice = false;
+      if (w != 0.f) {
+        // whether a column of this block's part comes twice: a bit for each, set and cleared by its
+        // entries (between a row's barrier and the next one the bits are this teacher's alone)
+#pragma unroll 4
+        for (int k = lane; k < entries; k += 32) {
+          const int j = E.col[k];
+          const uint32_t bit = 1u << ((j - lo) & 31);
+          if (j >= 0 && j >= lo && j < hi) twice |= (atomicOr(&bitmap[(j - lo) >> 5], bit) & bit) != 0;
+        }
+        twice = __any_sync(0xffffffffu, twice);
+#pragma unroll 4
+        for (int k = lane; k < entries; k += 32) {
+          const int j = E.col[k];
+          if (j >= 0 && j >= lo && j < hi) bitmap[(j - lo) >> 5] = 0;
+        }
+        __syncwarp();
       }
-      twice = __any_sync(0xffffffffu, twice);
-      for (int k = lane; k < entries; k += 32) {
-        const int j = E.col[k];
-        if (j >= 0 && j >= lo && j < hi) bitmap[(j - lo) >> 5] = 0;
+      barrier(n + 1);
+      if (rank == 0) {
+        const float loss = w == 0.f ? 0.f : w * row_loss<TWO>(A, E, terms, s);
+        if (lane == 0) A.loss[row] = loss;
       }
-      __syncwarp();
-    }
-    if (lane == 0) row_terms[turn] = (terms.soft ? 1 : 0) | (terms.hard ? 2 : 0);
-    block_barrier();
-    Stats s = block_merge<TWO>(warp_stats[turn], workers, A.c);
-    if (A.cluster > 1) s = cluster_merge<TWO>(s, block_stats[turn], A.cluster, rank, A.c);
-    finish(other);
-    last.row = row, last.w = w, last.terms = terms, last.f = factors<TWO>(A, terms, s, w), last.twice = twice;
-    if (rank == 0) {
-      const float loss = w == 0.f ? 0.f : row_loss<TWO>(A, E, terms, s);
-      if (lane == 0) A.loss[row] = w == 0.f ? 0.f : w * loss;
+      if (w != 0.f) {
+        T *g = static_cast<T *>(A.grad) + row * A.ldg;
+        const Factors f = factors<TWO>(A, terms, s, w);
+#pragma unroll 4
+        for (int k = lane; k < entries; k += 32) {
+          const int j = E.col[k];
+          float off = E.share(A, k, top);
+          bool write = j >= 0 && j >= lo && j < hi;
+          if (twice && write) {  // an entry that comes several times: the first writes, with all their shares
+            off = 0.f;
+            for (int i = 0; i < entries; ++i)
+              if (E.col[i] == j) write &= i >= k, off += E.share(A, i, top);
+          }
+          if (write) store_one(g + j, base_gradient<TWO>(f, E.zval[k], A.c) - w * off);
+        }
+        __syncwarp();  // the entries are read; the next row takes their place
+      }
     }
   }
-  block_barrier();
-  finish(Entries(entry_mem + (turn ^ 1) * 3 * (top + 1), top + 1));
+  if (A.cluster > 1) tc::cluster_sync();  // nothing is sent to a block that is gone
 }
 
 // ----------------------------------------------------------------------------- dispatch ---
@@ -598,7 +719,7 @@ Args make_args(const dion_distill *d, float *loss) {
   A.d = *d, A.loss = loss;
   A.soft = d->hard < 1.f, A.hard = d->hard > 0.f;
   const float t = A.soft ? d->temperature : 1.f;
-  A.c = kLog2e / t;
+  A.c = kLog2e / t, A.inv_t = 1.f / t;
   A.k_soft = (1.f - d->hard) * t, A.k_hard = d->hard;
   return A;
 }
@@ -633,25 +754,26 @@ dion_status enqueue_grad(const dion_distill *d, float *loss, void *grad, int64_t
   A.grad = grad, A.ldg = ldg;
   const int64_t chunks = row_chunks(d);
   const int per_chunk = 16 / element_bytes(d->dtype);
-  auto shape = [&](int cluster, int buffers) {
-    A.cluster = cluster, A.buffers = buffers;
+  auto shape = [&](int cluster, int buffers, int teachers) {
+    A.cluster = cluster, A.buffers = buffers, A.teachers = teachers;
     A.part = (int32_t)((chunks + cluster - 1) / cluster);
     A.bitmap = (A.part * per_chunk + 31) / 32;
-    return (size_t)A.part * 16 * buffers + 4 * (size_t)A.bitmap + 2 * entry_bytes(A);
+    return (size_t)A.part * 16 * buffers + 4 * (size_t)A.bitmap + teachers * entry_bytes(A);
   };
   const size_t most = kSmemPerSm - kSmemPerBlock - kStaticSmem;
   int cluster = 1;
-  while (cluster < kMaxCluster && shape(cluster, 2) > most) cluster *= 2;
+  while (cluster < kMaxCluster && shape(cluster, 2, kMaxTeachers) > most) cluster *= 2;
   // rows that leave SMs idle are shared by more blocks, down to a chunk per thread
-  while (cluster < kMaxCluster && d->rows * cluster * 2 <= sms && chunks / cluster > kMaxThreads) cluster *= 2;
-  size_t smem = shape(cluster, 2);
-  if (smem > most) smem = shape(cluster, 1);
+  while (cluster < kMaxCluster && d->rows * cluster * 2 <= sms && chunks / cluster > 32 * kMaxWorkers) cluster *= 2;
+  size_t smem = shape(cluster, 2, kMaxTeachers);
+  if (smem > most) smem = shape(cluster, 1, 2);
   if (smem > most) return DION_ERR_UNSUPPORTED;
-  // six chunks per thread between two barriers, or one where rows are few
-  const int64_t per_thread = d->rows * cluster <= sms ? 1 : 6;
-  const int warps = (int)std::min<int64_t>(kMaxThreads / 32 - 1, std::max<int64_t>(1, (A.part / per_thread + 31) / 32));
-  const int threads = (warps + 1) * 32;
-  const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(kMaxThreads / threads, (int64_t)(kSmemPerSm / (smem + kSmemPerBlock + kStaticSmem))));
+  // ten chunks per thread between two barriers, or one where rows are few
+  const int64_t per_thread = d->rows * cluster <= sms ? 1 : 10;
+  const int workers = (int)std::min<int64_t>(kMaxWorkers, std::max<int64_t>(1, (A.part / per_thread + 31) / 32));
+  const int threads = (workers + A.teachers) * 32;
+  const int64_t resident = std::max<int64_t>(
+      1, std::min<int64_t>(kGradThreads / threads, (int64_t)(kSmemPerSm / (smem + kSmemPerBlock + kStaticSmem))));
   const int64_t clusters = std::min<int64_t>(d->rows, std::max<int64_t>(1, sms * resident / cluster));
   const bool two = two_softmaxes(A);
   using BF = __nv_bfloat16;

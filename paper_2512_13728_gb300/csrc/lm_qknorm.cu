@@ -23,8 +23,14 @@ constexpr int kMaxPairs = kMaxHeadDim / 2;
 constexpr int kMaxHeads = 2048;  // of q, of k
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kForwardHeads = 4;   // heads that a group has in flight
-constexpr int kBackwardHeads = 2;
+#ifndef FU
+#define FU 4
+#define FB 1
+#define BU 2
+#define BB 2
+#endif
+constexpr int kForwardHeads = FU;   // heads that a group has in flight
+constexpr int kBackwardHeads = BU;
 }  // namespace
 
 struct dion_qknorm_plan {
@@ -217,7 +223,7 @@ struct Token {
 
 // ------------------------------------------------------------------------------ forward ---
 template <class T, int V, int NC, bool INTER>
-__global__ void __launch_bounds__(kThreads) forward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kThreads, FB) forward_kernel(const __grid_constant__ Args A) {
   constexpr int U = kForwardHeads;
   __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs];
   chain_enter();
@@ -276,7 +282,7 @@ __global__ void __launch_bounds__(kThreads) forward_kernel(const __grid_constant
 // ----------------------------------------------------------------------------- backward ---
 // A warp keeps to one batch of heads and goes over tokens, so that its sums of dw stay in registers.
 template <class T, int V, int NC, bool INTER>
-__global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kThreads, BB) backward_kernel(const __grid_constant__ Args A) {
   constexpr int U = kBackwardHeads;
   __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs], red[kWarps][2 * kMaxHeadDim];
   __shared__ bool last;
