@@ -22,9 +22,9 @@ using namespace cd::lm;
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMaxWorkers = 20, kMaxTeachers = 4;  // warps of the gradient's blocks
-constexpr int kGradThreads = 32 * (kMaxWorkers + kMaxTeachers);
-constexpr int kLossThreads = 512;
+constexpr int kMaxWorkers = 12, kMaxTeachers = 3;  // warps of the gradient's blocks
+constexpr int kGradThreads = 512;                   // of a block; two blocks per SM
+constexpr int kLossThreads = 256;
 constexpr int kMaxCluster = 8;
 constexpr int kBatch = 4;  // of the teacher's entries that a lane loads together
 constexpr size_t kSmemPerSm = 227 * 1024, kSmemPerBlock = 1024;  // of an SM; what the system takes of each block's
@@ -35,8 +35,7 @@ struct Args {
   float *loss;
   void *grad;
   int64_t ldg;
-  int32_t cluster, part;  // blocks per row, chunks of 16 bytes per block
-  int32_t buffers;        // rows in shared memory: 2, or 1 where two do not fit
+  int32_t cluster, part;  // blocks per row, chunks of 16 bytes per block (a multiple of 8)
   int32_t bitmap;         // words
   int32_t teachers;       // warps for the teacher's entries
   float c, inv_t;         // log2(e) / temperature of the first softmax, 1 / temperature
@@ -172,28 +171,31 @@ __device__ __forceinline__ float load_any(const void *p, int32_t dtype, int64_t 
   return dtype == DION_DTYPE_FP32 ? static_cast<const float *>(p)[i] : load_one(static_cast<const __nv_bfloat16 *>(p) + i);
 }
 
-// One row as a block sees it: chunks of 16 bytes at multiples of 16, of which the block's are [lo, hi).
-// The first and the last chunk of a row may be only partly its own (edges); thread t of the block's
-// `threads` has chunks lo + t, lo + t + threads, ...
+// One row as a block sees it: chunks of 16 bytes, counted from the multiple of 128 bytes at or before
+// the row, so that a warp's 32 chunks are whole lines; the block's are [lo, hi).  The first and the last
+// chunk of a row may be only partly its own (edges).  Thread t of the block's `threads` has chunks
+// base + t, base + t + threads, ... from lo on.
 template <class T>
 struct Row {
   static constexpr int N = 16 / sizeof(T);
   const T *z;
-  int lead;  // elements before the row in its first chunk
-  int vocab, lo, hi;
-  int whole_hi;     // end of the block's chunks before a last edge
-  bool first_edge;  // chunk lo is an edge at the row's beginning
+  int lead;  // elements between the line's beginning and the row's
+  int vocab, base, lo, hi;
+  int whole_lo, whole_hi;  // the block's chunks that are no edges
   __device__ __forceinline__ Row(const Args &A, int64_t row, int rank) {
     z = static_cast<const T *>(A.d.logits) + row * A.d.ld;
-    lead = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T));
+    lead = (int)(reinterpret_cast<uintptr_t>(z) % 128 / sizeof(T));
     vocab = (int)A.d.vocab;
-    lo = rank * A.part;
-    hi = min(lo + A.part, (lead + vocab + N - 1) / N);
+    base = rank * A.part;
+    lo = max(base, lead / N);
+    hi = min(base + A.part, (lead + vocab + N - 1) / N);
+    whole_lo = max(lo, (lead + N - 1) / N);
     whole_hi = min(hi, (lead + vocab) / N);
-    first_edge = lead > 0 && rank == 0;
   }
+  __device__ __forceinline__ int first(int t, int threads) const { return base + t + (base + t < lo ? threads : 0); }
   __device__ __forceinline__ int column(int chunk) const { return chunk * N - lead; }
   __device__ __forceinline__ const uint4 *at(int chunk) const { return reinterpret_cast<const uint4 *>(z + column(chunk)); }
+  __device__ __forceinline__ bool whole(int chunk) const { return chunk >= whole_lo && chunk < whole_hi; }
   // an edge's own elements, with -infinity around them
   __device__ __forceinline__ uint4 edge(int chunk) const {
     uint4 raw;
@@ -358,7 +360,7 @@ __device__ __forceinline__ void send(const Stats &s, Stats *blocks, int to, int 
 // --------------------------------------------------------------------------------- loss ---
 // One row per cluster, straight from global memory; the last warp has the teacher's entries.
 template <class T, bool TWO>
-__global__ void __launch_bounds__(kLossThreads, 3) loss_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kLossThreads, 6) loss_kernel(const __grid_constant__ Args A) {
   extern __shared__ float entry_mem[];
   __shared__ Stats warp_stats[32], block_stats[kMaxCluster];
   const Entries E(entry_mem, (A.soft ? (int)A.d.top : 0) + 1);
@@ -383,9 +385,9 @@ __global__ void __launch_bounds__(kLossThreads, 3) loss_kernel(const __grid_cons
   } else {
     const Row<T> r(A, row, rank);
     Stats s{-INFINITY, 0.f, 0.f};
-    int c = r.lo + tid;
+    int c = r.first(tid, threads);
     Chunk<T> one[1];
-    if (tid == 0 && r.first_edge) {
+    if (c < r.whole_lo && c < r.hi) {
       one[0].raw = r.edge(c);
       take<T, 1, TWO>(one, s, A.c);
       c += threads;
@@ -461,7 +463,7 @@ __device__ __forceinline__ bool wait_stats(uint64_t *bar, uint32_t parity) {
 // writes that row's entries over what the workers wrote there).  So a teacher has `teachers` - 1 rows of
 // time for its loads and softmax, and a worker meets one barrier per row.
 template <class T, bool TWO>
-__global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kGradThreads, 2) grad_kernel(const __grid_constant__ Args A) {
   constexpr int N = 16 / sizeof(T);
   extern __shared__ uint4 smem[];
   __shared__ Stats warp_stats[2][32], block_stats[2][kMaxCluster];
@@ -473,7 +475,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_cons
   const int rank = (int)(blockIdx.x % (unsigned)A.cluster), top = A.soft ? (int)d.top : 0, entries = top + (A.hard ? 1 : 0);
   const int64_t first = blockIdx.x / (unsigned)A.cluster, stride = gridDim.x / (unsigned)A.cluster;
   const int rows = (int)((d.rows - first + stride - 1) / stride);  // of this block
-  uint32_t *bitmap = reinterpret_cast<uint32_t *>(smem + (size_t)A.buffers * A.part);
+  uint32_t *bitmap = reinterpret_cast<uint32_t *>(smem + A.part);
   float *entry_mem = reinterpret_cast<float *>(bitmap + A.bitmap);
   for (int i = tid; i < A.bitmap; i += blockDim.x) bitmap[i] = 0;
   if (A.cluster > 1) {
@@ -504,37 +506,28 @@ __global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_cons
   };
 
   if (warp < workers) {
-    auto start_copy = [&](const Row<T> &r, uint4 *to) {  // this thread's chunks of a row
-      int c = r.lo + tid;
-      to += tid;
-      if (tid == 0 && r.first_edge) *to = r.edge(c), c += threads, to += threads;
-      const uint4 *from = r.at(c);
-#pragma unroll 4
-      for (; c < r.whole_hi; c += threads, from += threads, to += threads)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to)), "l"(from) : "memory");
-      if (c < r.hi) *to = r.edge(c);
+    auto copy = [&](const Row<T> &r, int c) {  // chunk c of a row into its place
+      uint4 *to = smem + (c - r.base);
+      if (r.whole(c))
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(to)), "l"(r.at(c)) : "memory");
+      else
+        *to = r.edge(c);
     };
     float w = weight(first), w_next = weight(first + stride);
     Row<T> r(A, first, rank);
-    if (w != 0.f) start_copy(r, smem);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (w != 0.f)
+      for (int c = r.first(tid, threads); c < r.hi; c += threads) copy(r, c);
     for (int n = 0; n < rows; ++n) {
       const int64_t row = first + n * stride;
       const float w_after = weight(row + 2 * stride);
-      const uint4 *mine = smem + (A.buffers > 1 && (n & 1) ? A.part : 0) + tid;
       const Row<T> r_next(A, row + stride, rank);
       T *g = static_cast<T *>(A.grad) + row * A.ldg;
-      if (A.buffers > 1) {
-        if (w_next != 0.f) start_copy(r_next, smem + (n & 1 ? 0 : A.part));
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
-      } else {
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
       Stats s{-INFINITY, 0.f, 0.f};
+      const int c_first = r.first(tid, threads);
       if (w != 0.f) {
-        int left = r.hi - r.lo - tid;
-        const uint4 *from = mine;
+        int left = r.hi - c_first;
+        const uint4 *from = smem + (c_first - r.base);
         for (; left > 3 * threads; left -= 4 * threads, from += 4 * threads) {
           Chunk<T> v[4];
 #pragma unroll
@@ -555,7 +548,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_cons
       const Factors f = factors<TWO>(A, RowTerms{(t & 1) != 0, (t & 2) != 0}, s, w);
       const bool zeros = w == 0.f || t == 0;
       // whole chunks are stored where the gradient's row sits at the same place within 16 bytes
-      const bool same_place = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T)) == r.lead;
+      const bool same_place = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T)) == r.lead % N;
       const uint64_t c2 = pack2(A.c, A.c), m2 = pack2(-f.m, -f.m), k2 = pack2(f.k, f.k);
       const uint64_t l2 = pack2(kLog2e, kLog2e), k12 = pack2(f.k1, f.k1);
       auto gradient = [&](const uint4 &raw, float(&v)[N]) {
@@ -574,36 +567,47 @@ __global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_cons
           unpack2(y, v[2 * i], v[2 * i + 1]);
         }
       };
-      auto single = [&](int c, const uint4 &raw) {  // element by element
-        float v[N];
-        gradient(raw, v);
+      // a chunk whose row's or next row's place needs a look: element by element, then the next row's
+      const bool more = w_next != 0.f;
+      auto single = [&](int c) {
+        if (c >= r.lo && c < r.hi) {
+          float v[N];
+          gradient(smem[c - r.base], v);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const int j = r.column(c) + e;
-          if (j >= 0 && j < r.vocab) store_one(g + j, zeros ? 0.f : v[e]);
-        }
-      };
-      int c = r.lo + tid;
-      const uint4 *from = mine;
-      if (tid == 0 && r.first_edge) single(c, *from), c += threads, from += threads;
-      if (same_place) {
-        uint4 *to = reinterpret_cast<uint4 *>(g + r.column(c));
-        if (zeros) {
-          for (; c < r.whole_hi; c += threads, from += threads, to += threads) *to = make_uint4(0, 0, 0, 0);
-        } else {
-#pragma unroll 2
-          for (; c < r.whole_hi; c += threads, from += threads, to += threads) {
-            float v[N];
-            gradient(*from, v);
-            store_vec<T, N>(reinterpret_cast<T *>(to), v);
+          for (int e = 0; e < N; ++e) {
+            const int j = r.column(c) + e;
+            if (j >= 0 && j < r.vocab) store_one(g + j, zeros ? 0.f : v[e]);
           }
         }
+        if (more && c >= r_next.lo && c < r_next.hi) copy(r_next, c);
+      };
+      // each chunk's place takes the next row's chunk as soon as its gradient is stored
+      int c = r.base + tid;
+      const int end = max(r.hi, r_next.hi), both_hi = more ? min(r.whole_hi, r_next.whole_hi) : r.whole_hi;
+      if (c < max(r.whole_lo, r_next.whole_lo)) single(c), c += threads;
+      if (same_place) {
+        uint4 *place = smem + (c - r.base), *to = reinterpret_cast<uint4 *>(g + r.column(c));
+        const uint4 *from = r_next.at(c);
+        auto refill = [&] {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(place)), "l"(from) : "memory");
+        };
+        auto put = [&] {
+          float v[N];
+          gradient(*place, v);
+          store_vec<T, N>(reinterpret_cast<T *>(to), v);
+        };
+        if (zeros) {
+          for (; c < both_hi; c += threads, place += threads, from += threads, to += threads) {
+            *to = make_uint4(0, 0, 0, 0);
+            if (more) refill();
+          }
+        } else if (more) {
+          for (; c < both_hi; c += threads, place += threads, from += threads, to += threads) put(), refill();
+        } else {
+          for (; c < both_hi; c += threads, place += threads, to += threads) put();
+        }
       }
-      for (; c < r.hi; c += threads, from += threads) single(c, *from);
-      if (A.buffers == 1 && n + 1 < rows) {
-        if (w_next != 0.f) start_copy(r_next, smem);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      }
+      for (; c < end; c += threads) single(c);
       w = w_next, w_next = w_after;
       r = r_next;
     }
@@ -725,7 +729,9 @@ Args make_args(const dion_distill *d, float *loss) {
 }
 // Two softmaxes only where both terms are there and differ in temperature.
 bool two_softmaxes(const Args &A) { return A.soft && A.hard && A.d.temperature != 1.f; }
-int64_t row_chunks(const dion_distill *d) { return d->vocab * element_bytes(d->dtype) / 16 + 2; }  // the most a row touches
+// The most chunks of a row, counted from its line's beginning.
+int64_t row_chunks(const dion_distill *d) { return (d->vocab * element_bytes(d->dtype) + 127) / 16 + 1; }
+int32_t part_of(int64_t chunks, int cluster) { return (int32_t)(((chunks + cluster - 1) / cluster + 7) / 8 * 8); }
 size_t entry_bytes(const Args &A) { return 12 * ((A.soft ? (size_t)A.d.top : 0) + 1); }
 
 dion_status enqueue_loss(const dion_distill *d, float *loss, cudaStream_t s) {
@@ -735,7 +741,7 @@ dion_status enqueue_loss(const dion_distill *d, float *loss, cudaStream_t s) {
   const int64_t chunks = row_chunks(d);
   A.cluster = 1;  // more blocks per row while the rows leave SMs idle and a thread has more than one round of chunks
   while (A.cluster < kMaxCluster && d->rows * A.cluster * 2 <= sms && chunks / A.cluster > 4 * kLossThreads) A.cluster *= 2;
-  A.part = (int32_t)((chunks + A.cluster - 1) / A.cluster);
+  A.part = part_of(chunks, A.cluster);
   const int threads = (int)std::min<int64_t>(kLossThreads, (A.part + 31) / 32 * 32 + 32);
   const size_t smem = entry_bytes(A);
   const int64_t grid = d->rows * A.cluster;
@@ -754,26 +760,26 @@ dion_status enqueue_grad(const dion_distill *d, float *loss, void *grad, int64_t
   A.grad = grad, A.ldg = ldg;
   const int64_t chunks = row_chunks(d);
   const int per_chunk = 16 / element_bytes(d->dtype);
-  auto shape = [&](int cluster, int buffers, int teachers) {
-    A.cluster = cluster, A.buffers = buffers, A.teachers = teachers;
-    A.part = (int32_t)((chunks + cluster - 1) / cluster);
+  auto shape = [&](int cluster, int teachers) {
+    A.cluster = cluster, A.teachers = teachers;
+    A.part = part_of(chunks, cluster);
     A.bitmap = (A.part * per_chunk + 31) / 32;
-    return (size_t)A.part * 16 * buffers + 4 * (size_t)A.bitmap + teachers * entry_bytes(A);
+    return (size_t)A.part * 16 + 4 * (size_t)A.bitmap + teachers * entry_bytes(A);
   };
-  const size_t most = kSmemPerSm - kSmemPerBlock - kStaticSmem;
-  int cluster = 1;
-  while (cluster < kMaxCluster && shape(cluster, 2, kMaxTeachers) > most) cluster *= 2;
+  const size_t taken = kSmemPerBlock + kStaticSmem;
+  int cluster = 1;  // so that two blocks share an SM: one works while the other waits
+  while (cluster < kMaxCluster && shape(cluster, kMaxTeachers) + taken > kSmemPerSm / 2) cluster *= 2;
   // rows that leave SMs idle are shared by more blocks, down to a chunk per thread
   while (cluster < kMaxCluster && d->rows * cluster * 2 <= sms && chunks / cluster > 32 * kMaxWorkers) cluster *= 2;
-  size_t smem = shape(cluster, 2, kMaxTeachers);
-  if (smem > most) smem = shape(cluster, 1, 2);
-  if (smem > most) return DION_ERR_UNSUPPORTED;
-  // ten chunks per thread between two barriers, or one where rows are few
-  const int64_t per_thread = d->rows * cluster <= sms ? 1 : 10;
-  const int workers = (int)std::min<int64_t>(kMaxWorkers, std::max<int64_t>(1, (A.part / per_thread + 31) / 32));
+  size_t smem = shape(cluster, kMaxTeachers);
+  if (smem + taken > kSmemPerSm) smem = shape(cluster, 2);
+  if (smem + taken > kSmemPerSm) return DION_ERR_UNSUPPORTED;
+  const int64_t by_smem = (int64_t)(kSmemPerSm / (smem + taken));
+  // about 32 warps per SM; with many blocks per SM no less than eight chunks per thread
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kMaxWorkers, 32 / by_smem - A.teachers));
+  const int workers = (int)std::min<int64_t>(want, std::max<int64_t>(1, (A.part / (d->rows * cluster <= sms ? 1 : 8) + 31) / 32));
   const int threads = (workers + A.teachers) * 32;
-  const int64_t resident = std::max<int64_t>(
-      1, std::min<int64_t>(kGradThreads / threads, (int64_t)(kSmemPerSm / (smem + kSmemPerBlock + kStaticSmem))));
+  const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(by_smem, 1024 / threads));
   const int64_t clusters = std::min<int64_t>(d->rows, std::max<int64_t>(1, sms * resident / cluster));
   const bool two = two_softmaxes(A);
   using BF = __nv_bfloat16;

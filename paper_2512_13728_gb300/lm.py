@@ -31,6 +31,7 @@ _DISTILL = Struct("@qqqPqPqPqPPiiiiff")
 # torch.cuda.current_stream builds a Stream object (2 us); this is the address alone
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _stream(index: int, stream: Optional[int], outputs_given: bool) -> int:
@@ -292,22 +293,13 @@ def _row_values(name: str, t, rows: int, index: int) -> int:
     return t.data_ptr()
 
 
-class _OnDevice:
-    """Makes a device current for a call, where it is not already (torch.cuda.device always takes 1 us)."""
-
-    __slots__ = ("index", "guard")
-
-    def __init__(self, index: int):
-        self.index, self.guard = index, None
-
-    def __enter__(self):
-        if torch.cuda.current_device() != self.index:
-            self.guard = torch.cuda.device(self.index)
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _on_device(index: int, call, *args) -> None:
+    """The call with that device current (torch.cuda.device takes 1 us also where it already is)."""
+    if _current_device() == index:
+        call(*args)
+    else:
+        with torch.cuda.device(index):
+            call(*args)
 
 
 def distill_loss(logits, ids, teacher, temperature: float = 1.0, labels=None, hard: float = 0.0, weights=None, out=None,
@@ -318,8 +310,7 @@ def distill_loss(logits, ids, teacher, temperature: float = 1.0, labels=None, ha
     args, index, rows = _distill(logits, ids, teacher, temperature, labels, hard, weights)
     s = _stream(index, stream, out is not None)
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device) if out is None else out
-    with _OnDevice(index):
-        native.dion_distill_loss(args, _row_values("the loss", loss, rows, index), s)
+    _on_device(index, native.dion_distill_loss, args, _row_values("the loss", loss, rows, index), s)
     return loss
 
 
@@ -337,6 +328,6 @@ def distill_loss_grad(logits, ids, teacher, temperature: float = 1.0, labels=Non
         if grad.dtype != logits.dtype or grad.shape != logits.shape:
             raise ValueError("the gradient must have the logits' shape and dtype")
     ldg = _ld("the gradient", grad, index, logits.shape[1])
-    with _OnDevice(index):
-        native.dion_distill_loss_grad(args, _row_values("the loss", loss, rows, index), grad.data_ptr(), ldg, s)
+    _on_device(index, native.dion_distill_loss_grad, args, _row_values("the loss", loss, rows, index), grad.data_ptr(), ldg,
+               s)
     return loss, grad
