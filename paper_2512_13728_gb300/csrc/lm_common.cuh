@@ -8,16 +8,19 @@
 namespace cd {
 namespace lm {
 
-// V elements of a row as fp32 values.  The address is a multiple of min(16, V * sizeof(T)) bytes.
+// V elements of a row as fp32 values, in one access.  The address is a multiple of V * sizeof(T) bytes (32
+// at most).
 template <class T, int V>
 __device__ __forceinline__ void load_vec(const T *p, float (&v)[V]) {
   if constexpr (sizeof(T) == 4) {
-    if constexpr (V % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const float4 x = *reinterpret_cast<const float4 *>(p + i);
-        v[i] = x.x, v[i + 1] = x.y, v[i + 2] = x.z, v[i + 3] = x.w;
-      }
+    if constexpr (V == 8) {
+      asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                   : "l"(__cvta_generic_to_global(p))
+                   : "memory");
+    } else if constexpr (V == 4) {
+      const float4 x = *reinterpret_cast<const float4 *>(p);
+      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
     } else if constexpr (V == 2) {
       const float2 x = *reinterpret_cast<const float2 *>(p);
       v[0] = x.x, v[1] = x.y;
@@ -52,9 +55,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 template <class T, int V>
 __device__ __forceinline__ void store_vec(T *p, const float (&v)[V]) {
   if constexpr (sizeof(T) == 4) {
-    if constexpr (V % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    if constexpr (V == 8) {
+      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(__cvta_generic_to_global(p)), "f"(v[0]),
+                   "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                   : "memory");
+    } else if constexpr (V == 4) {
+      *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
     } else if constexpr (V == 2) {
       *reinterpret_cast<float2 *>(p) = make_float2(v[0], v[1]);
     } else {
@@ -72,6 +78,35 @@ __device__ __forceinline__ void store_vec(T *p, const float (&v)[V]) {
       *p = __float2bfloat16_rn(v[0]);
   }
 }
+
+// V elements as they sit in memory.
+template <class T, int V>
+struct Raw {
+  static constexpr int kBytes = V * (int)sizeof(T);
+  uint32_t w[kBytes >= 4 ? kBytes / 4 : 1];
+  __device__ __forceinline__ void load(const T *p) {
+    if constexpr (kBytes == 32) {
+      asm volatile("ld.global.v8.u32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                   : "l"(__cvta_generic_to_global(p))
+                   : "memory");
+    } else if constexpr (kBytes == 16) {
+      const uint4 x = *reinterpret_cast<const uint4 *>(p);
+      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else if constexpr (kBytes == 8) {
+      const uint2 x = *reinterpret_cast<const uint2 *>(p);
+      w[0] = x.x, w[1] = x.y;
+    } else if constexpr (kBytes == 4) {
+      w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t *>(p);
+    }
+  }
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
+};
 
 // An index of either width; the caller bounds it.
 __device__ __forceinline__ int64_t load_index(const void *p, int32_t dtype, int64_t i) {

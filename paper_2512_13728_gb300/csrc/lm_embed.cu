@@ -3,12 +3,14 @@
 //   lookup    out[i] = s E[t_i]
 //   gradient  dE[v] (+)= s sum_{i : t_i = v} dy[i]
 //
-// The gradient sorts (token, position) pairs with a stable radix sort and then walks the merge of
-// two lists: the sorted entries and the ends of the table's rows.  Every warp takes an equal share of
+// The gradient sorts (token, position) pairs with a stable radix sort (up to 131072 tokens in one
+// cluster of blocks, whose shared memory holds them) and then walks the merge of two lists: the
+// sorted entries and the ends of the table's rows.  Every warp takes an equal share of
 // that merge for a slab of 256 columns, whatever the tokens are: a token that comes thousands of
 // times is split over warps, and the rows that no token names are zeroed along the way.  A row that
 // lies in several shares is added up from the shares' fp32 sums in a second small kernel, in order.
 #include "lm_common.cuh"
+#include "tc_common.cuh"
 
 #include <algorithm>
 #include <cmath>
@@ -26,6 +28,18 @@ constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSlab = 256;        // columns that a warp takes, 8 per lane
 constexpr int kWalkThreads = 256;
+#ifndef WB
+#define WB 4
+#endif
+#ifndef UR
+#define UR 16
+#endif
+#ifndef C1
+#define C1 4
+#endif
+#ifndef RC
+#define RC 0
+#endif
 
 }  // namespace
 
@@ -79,6 +93,19 @@ __device__ __forceinline__ uint32_t token_key(const void *tokens, int32_t dtype,
   return (t >= 0 && t < vocab) ? (uint32_t)t : (uint32_t)vocab;
 }
 
+// The lanes whose digit is this lane's: a ballot for each bit (match.any of a whole value takes several
+// times as long).
+__device__ __forceinline__ uint32_t lanes_with(uint32_t digit, int bits) {
+  uint32_t same = 0xffffffffu;
+#pragma unroll
+  for (int b = 0; b < 10; ++b) {
+    if (b >= bits) break;
+    const uint32_t one = __ballot_sync(0xffffffffu, (digit >> b) & 1);
+    same &= (digit >> b) & 1 ? one : ~one;
+  }
+  return same;
+}
+
 // Counts of each digit in each tile of kSortTile entries.  key == null: the first pass, from the tokens.
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t *key, const void *tokens, int32_t dtype,
                                                                   int64_t vocab, int64_t n, int shift, int bits,
@@ -120,7 +147,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const uint32_t 
     k[r] = in ? (key ? key[i] : token_key(tokens, dtype, i, vocab)) : 0u;
     p[r] = in ? (pos ? pos[i] : (uint32_t)i) : 0u;
     const uint32_t digit = in ? (k[r] >> shift) & (bins - 1) : (uint32_t)bins;  // entries past the end match each other only
-    const uint32_t same = __match_any_sync(0xffffffffu, digit);
+    const uint32_t same = lanes_with(digit, bits + 1);
     const int leader = __ffs(same) - 1;
     uint32_t before = 0;
     if (in && lane == leader) {
@@ -181,30 +208,154 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const uint32_t 
   }
 }
 
+// The same sort of up to cluster x 1024 x I entries in one launch: block b holds entries [b 1024 I, (b + 1)
+// 1024 I), warp w of it 32 I of them in I rounds of 32.  A pass counts the digits of each warp, adds up
+// the counts over warps and (through distributed shared memory) over blocks, and writes each entry
+// to its place in the block that holds it next; the last pass writes to global memory.
+constexpr int kClusterThreads = 1024;
+constexpr int kClusterWarps = kClusterThreads / 32;
+constexpr int kMaxClusterItems = 16, kMaxClusterBlocks = 8;
+constexpr size_t kClusterCounts = sizeof(uint16_t) * kClusterWarps * kMaxBins;
+
+__device__ __forceinline__ uint32_t load_cluster(const uint32_t *p, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(tc::cluster_addr(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ void store_cluster(uint2 *p, uint32_t rank, uint2 v) {
+  asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(tc::cluster_addr(p, rank)), "r"(v.x), "r"(v.y) : "memory");
+}
+
+template <int I>
+__global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const void *tokens, int32_t dtype, int64_t vocab,
+                                                                          int32_t n, int passes, int bits, int blocks,
+                                                                          uint32_t *key_out, uint32_t *pos_out) {
+  extern __shared__ __align__(16) char sort_mem[];
+  uint16_t(*count)[kMaxBins] = reinterpret_cast<uint16_t(*)[kMaxBins]>(sort_mem);  // [warp][digit]
+  uint2 *entry = reinterpret_cast<uint2 *>(sort_mem + kClusterCounts);             // [1024 I]: key, position
+  __shared__ uint32_t total[2][kMaxBins], first[kMaxBins], warp_total[kMaxBins / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bins = 1 << bits;
+  const uint32_t rank = blocks > 1 ? tc::cluster_ctarank() : 0;
+  constexpr int kHeld = kClusterThreads * I;
+  const int begin = warp * 32 * I + lane;  // this lane's first entry in the block
+  chain_enter();
+  uint32_t k[I], p[I], place[I];
+#pragma unroll
+  for (int r = 0; r < I; ++r) {
+    const int64_t i = (int64_t)rank * kHeld + begin + r * 32;
+    p[r] = (uint32_t)i;
+    k[r] = i < n ? token_key(tokens, dtype, i, vocab) : 0xffffffffu;  // behind everything
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * bits;
+    for (int b = tid; b < kClusterWarps * kMaxBins / 2; b += kClusterThreads) reinterpret_cast<uint32_t *>(count)[b] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < I; ++r) {
+      const uint32_t digit = (k[r] >> shift) & (bins - 1);
+      const uint32_t same = lanes_with(digit, bits);
+      const int leader = __ffs(same) - 1;
+      uint32_t before = 0;
+      if (lane == leader) {
+        before = count[warp][digit];
+        count[warp][digit] = (uint16_t)(before + __popc(same));
+      }
+      place[r] = __shfl_sync(0xffffffffu, before, leader) + __popc(same & ((1u << lane) - 1));
+      __syncwarp();
+    }
+    __syncthreads();
+    uint32_t sum = 0, mine = 0, all = 0;  // of digit `tid`: of this block; of the blocks before; of all blocks
+    if (tid < bins) {
+#pragma unroll 8
+      for (int w = 0; w < kClusterWarps; ++w) {
+        const uint32_t c = count[w][tid];
+        count[w][tid] = (uint16_t)sum;
+        sum += c;
+      }
+      total[pass & 1][tid] = sum;
+    }
+    if (blocks > 1) {
+      tc::cluster_sync();
+      if (tid < bins)
+        for (int b = 0; b < blocks; ++b) {
+          const uint32_t c = load_cluster(&total[pass & 1][tid], b);
+          all += c;
+          if (b < (int)rank) mine += c;
+        }
+    } else {
+      all = sum;
+    }
+    uint32_t scan = all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, scan, o);
+      if (lane >= o) scan += x;
+    }
+    if (lane == 31 && warp < kMaxBins / 32) warp_total[warp] = scan;
+    __syncthreads();
+    if (tid < bins) {
+      uint32_t at = scan - all + mine;
+      for (int w = 0; w < warp; ++w) at += warp_total[w];
+      first[tid] = at;
+    }
+    __syncthreads();
+    const bool last = pass == passes - 1;
+#pragma unroll
+    for (int r = 0; r < I; ++r) {
+      const uint32_t digit = (k[r] >> shift) & (bins - 1);
+      const uint32_t at = first[digit] + count[warp][digit] + place[r];
+      if (!last) {
+        const uint32_t to = at / kHeld;
+        if (blocks > 1)
+          store_cluster(&entry[at - to * kHeld], to, make_uint2(k[r], p[r]));
+        else
+          entry[at] = make_uint2(k[r], p[r]);
+      } else if (at < (uint32_t)n) {
+        key_out[at] = k[r];
+        pos_out[at] = p[r];
+      }
+    }
+    if (!last) {
+      if (blocks > 1)
+        tc::cluster_sync();
+      else
+        __syncthreads();
+#pragma unroll
+      for (int r = 0; r < I; ++r) {
+        const uint2 e = entry[begin + r * 32];
+        k[r] = e.x, p[r] = e.y;
+      }
+    }
+  }
+  if (blocks > 1) tc::cluster_sync();  // no block reads the counts of one that is gone
+}
+
 // --------------------------------------------------------------------------------- walk ---
 struct Walk {
   const uint32_t *key, *pos;  // sorted entries
-  int64_t n, vocab, dim, ldg, ldd, parts, slabs, share;
+  int64_t ldg, ldd, share;
+  int32_t n, vocab, dim, parts, slabs;
+  int32_t row_cost;  // of a row's end in the merge, in entries
   float scale;
   float *head, *tail;
   int32_t *head_row, *tail_row;
 };
 
-// Entries of the first d items of the merge.  Entry j comes behind j entries and key[j] row ends, so
-// its place is j + key[j]; when accumulating there are no row ends in the merge and it is j.
+// Entries of the first d units of the merge.  Entry j comes behind j entries and key[j] row ends, so it
+// begins at j + cost key[j]; when accumulating there are no row ends in the merge and it is j.
 // Entries outside the table have places behind the last row end.
 template <bool ACC>
-__device__ __forceinline__ int64_t entries_before(const uint32_t *key, int64_t n, int64_t d) {
-  if (ACC) return d < n ? d : n;
+__device__ __forceinline__ int entries_before(const Walk &w, int64_t d) {
+  if (ACC) return (int)(d < w.n ? d : w.n);
   const int lane = threadIdx.x & 31;
-  int64_t lo = 0, hi = n < d ? n : d;  // the answer lies in [lo, hi]; 33-way search
+  int lo = 0, hi = (int)(w.n < d ? w.n : d);  // the answer lies in [lo, hi]; 33-way search
   while (hi > lo) {
-    const int64_t step = (hi - lo + 32) / 33;
-    const int64_t j = lo + (lane + 1) * step - 1;  // probe: is entry j among the first d items?
-    const bool in = j < hi && j + (int64_t)key[j] < d;
+    const int step = (hi - lo + 32) / 33;
+    const int j = lo + (lane + 1) * step - 1;  // probe: is entry j among the first d units?
+    const bool in = j < hi && j + (int64_t)w.key[j] * w.row_cost < d;
     const int hits = __popc(__ballot_sync(0xffffffffu, in));
-    const int64_t l2 = lo + hits * step, h2 = lo + (hits + 1) * step - 1;
-    lo = l2;
+    const int h2 = lo + (hits + 1) * step - 1;
+    lo += hits * step;
     hi = hits < 32 && h2 < hi ? h2 : hi;
   }
   return lo;
@@ -212,125 +363,162 @@ __device__ __forceinline__ int64_t entries_before(const uint32_t *key, int64_t n
 
 // One warp: a part of the merge, a slab of columns.
 template <class TG, class TD, int V, bool ACC>
-__global__ void __launch_bounds__(kWalkThreads) walk_kernel(const Walk w, const TG *grad, TD *dst) {
+__global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_constant__ Walk w, const TG *grad, TD *dst) {
+  constexpr int C = 8 / V;
+  constexpr int U = 4 * UR / (C * (int)sizeof(Raw<TG, V>));  // rows loaded together
   chain_enter();
   const int lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * (kWalkThreads / 32) + (threadIdx.x >> 5);
-  const int64_t part = unit / w.slabs, slab = unit - part * w.slabs;
+  const int unit = blockIdx.x * (kWalkThreads / 32) + (threadIdx.x >> 5), part = unit / w.slabs, slab = unit - part * w.slabs;
   if (part >= w.parts) return;
-  constexpr int C = 8 / V;
-  const int64_t c0 = slab * kSlab + lane * V;
+  const int c0 = slab * kSlab + lane * V;
   const int64_t d0 = part * w.share, d1 = d0 + w.share;
-  int64_t j = entries_before<ACC>(w.key, w.n, d0);
-  const int64_t j1 = entries_before<ACC>(w.key, w.n, d1);
+  int j = entries_before<ACC>(w, d0);
+  const int j1 = entries_before<ACC>(w, d1);
+  // accumulating: the row of the entries at hand, -1 before the first; else the rows that end in this part
+  int row = -1, row_end = 0;
+  if (!ACC) {
+    row = (int)min((d0 - j + w.row_cost - 1) / w.row_cost, (int64_t)w.vocab);
+    row_end = (int)min((d1 - j1 + w.row_cost - 1) / w.row_cost, (int64_t)w.vocab);
+  }
+  // the part's first row, where it began in an earlier part: its sums go to the join
+  const int first = ACC ? (j < j1 ? (int)w.key[j] : w.vocab) : row;
+  const int begun = j > 0 && first < w.vocab && (int)w.key[j - 1] == first ? first : -1;
+  const int64_t partial = (int64_t)unit * kSlab + lane * V;  // where the part's sums go
+  const TG *src = grad + c0;
+  TD *out = dst + c0;
   float acc[C][V];
-  auto clear = [&] {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+  for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[c][e] = 0.f;
-  };
+    for (int e = 0; e < V; ++e) acc[c][e] = 0.f;
   auto put_partial = [&](float *to) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) store_vec<float, V>(to + (part * w.slabs + slab) * kSlab + c * 32 * V + lane * V, acc[c]);
+    for (int c = 0; c < C; ++c) store_vec<float, V>(to + partial + c * 32 * V, acc[c]);
   };
-  auto put_row = [&](int64_t row) {
+  auto end_row = [&](int r) {
+    TD *to = out + r * w.ldd;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if (c0 + c * 32 * V >= w.dim) break;
-      float v[V];
-      TD *to = dst + row * w.ldd + c0 + c * 32 * V;
-      if (ACC) load_vec<TD, V>(to, v);
+      if (r == begun) {
+        store_vec<float, V>(w.head + partial + c * 32 * V, acc[c]);
+      } else if (c0 + c * 32 * V < w.dim) {
+        float v[V];
+        if (ACC) load_vec<TD, V>(to + c * 32 * V, v);
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = ACC ? fmaf(w.scale, acc[c][e], v[e]) : w.scale * acc[c][e];
-      store_vec<TD, V>(to, v);
+        for (int e = 0; e < V; ++e) v[e] = ACC ? fmaf(w.scale, acc[c][e], v[e]) : w.scale * acc[c][e];
+        store_vec<TD, V>(to + c * 32 * V, v);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[c][e] = 0.f;
     }
   };
-  auto add = [&](int64_t at) {
-    const TG *from = grad + (int64_t)w.pos[at] * w.ldg + c0;
+  int done = j;  // entries of the table so far
+  for (; j < j1; j += 32) {
+    // 32 entries' keys and positions, one per lane
+    const int key = j + lane < j1 ? (int)w.key[j + lane] : w.vocab, pos = j + lane < j1 ? (int)w.pos[j + lane] : 0;
+    for (int e0 = 0; e0 < 32 && e0 < j1 - j; e0 += U) {
+      Raw<TG, V> raw[U][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (c0 + c * 32 * V >= w.dim) break;
-      float v[V];
-      load_vec<TG, V>(from + c * 32 * V, v);
+      for (int u = 0; u < U; ++u) {
+        const int at = __shfl_sync(0xffffffffu, pos, e0 + u), k = __shfl_sync(0xffffffffu, key, e0 + u);
+        const TG *from = src + at * w.ldg;
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[c][e] += v[e];
-    }
-  };
-  clear();
-  int64_t head_row = -1, tail_row = -1;
-  if (ACC) {
-    // rows end where the key changes; the part's last row goes on where the next entry has its key
-    while (j < j1 && w.key[j] < w.vocab) {
-      const int64_t row = w.key[j];
-      const bool begun = j > 0 && w.key[j - 1] == row;
-      while (j < j1 && w.key[j] == row) add(j++);
-      if (j == j1 && j < w.n && w.key[j] == row) {
-        put_partial(w.tail);
-        tail_row = row;
-      } else if (begun) {
-        put_partial(w.head);
-        head_row = row;
-      } else {
-        put_row(row);
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+          for (uint32_t &x : raw[u][c].w) x = 0;
+          if (k < w.vocab && c0 + c * 32 * V < w.dim) raw[u][c].load(from + c * 32 * V);
+        }
       }
-      clear();
-    }
-  } else {
-    const int64_t i0 = d0 - j < w.vocab ? d0 - j : w.vocab, i1 = d1 - j1 < w.vocab ? d1 - j1 : w.vocab;
-    const bool begun = j > 0 && i0 < w.vocab && w.key[j - 1] == i0;
-    for (int64_t row = i0; row < i1; ++row) {
-      while (j < j1 && w.key[j] == row) add(j++);
-      if (row == i0 && begun) {
-        put_partial(w.head);
-        head_row = row;
-      } else {
-        put_row(row);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = __shfl_sync(0xffffffffu, key, e0 + u);
+        if (k >= w.vocab) break;  // the part's end, or entries outside the table: those come last
+        ++done;
+        if (ACC) {
+          if (row >= 0 && row != k) end_row(row);
+          row = k;
+        } else {
+          for (; row < k; ++row) end_row(row);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[c][e] += raw[u][c].at(e);
       }
-      clear();
-    }
-    if (j < j1 && i1 < w.vocab) {
-      while (j < j1) add(j++);
-      put_partial(w.tail);
-      tail_row = i1;
     }
   }
+  int tail = -1;  // a row that goes on in the next part
+  if (ACC) {
+    if (row >= 0 && done < w.n && (int)w.key[done] == row)
+      tail = row;
+    else if (row >= 0)
+      end_row(row);
+  } else {
+    for (; row < row_end; ++row) end_row(row);
+    if (row < w.vocab && j1 > 0 && (int)w.key[j1 - 1] == row) tail = row;
+  }
+  if (tail >= 0) put_partial(w.tail);
   if (slab == 0 && lane == 0) {
-    w.head_row[part] = (int32_t)head_row;
-    w.tail_row[part] = (int32_t)tail_row;
+    w.head_row[part] = begun == tail ? -1 : begun;
+    w.tail_row[part] = tail;
   }
 }
 
-// Rows that several parts have sums of: one block per part and slab; where the part ends such a row,
-// the sums are added in the order of the parts and the row is written.
+// Rows that several parts have sums of: a block per part and slab; where the part ends such a row, the
+// warps add up runs of the parts' sums, and the first warp those, in order, and writes the row.
 template <class TD, bool ACC>
-__global__ void __launch_bounds__(kSlab) join_kernel(const Walk w, TD *dst) {
+__global__ void __launch_bounds__(kWalkThreads) join_kernel(const __grid_constant__ Walk w, TD *dst) {
+  constexpr int kWarps = kWalkThreads / 32;
+  __shared__ float sums[kWarps][kSlab];
   chain_enter();
-  const int64_t part = blockIdx.x / w.slabs, slab = blockIdx.x - part * w.slabs;
-  const int64_t row = w.head_row[part];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = blockIdx.x / w.slabs, slab = blockIdx.x - part * w.slabs;
+  const int row = w.head_row[part];
   if (row < 0) return;
-  int64_t from = part;
-  while (from > 0 && w.tail_row[from - 1] == row) --from;
-  const int64_t col = slab * kSlab + threadIdx.x;
+  int from = part;  // the first of the parts that hold the row, 32 looked at together
+  for (bool more = true; more;) {
+    const int q = from - 1 - lane;
+    const uint32_t holds = __ballot_sync(0xffffffffu, q >= 0 && w.tail_row[q] == row);
+    const int run = holds == 0xffffffffu ? 32 : __ffs(~holds) - 1;
+    from -= run;
+    more = run == 32;
+  }
+  const int each = (part - from + kWarps) / kWarps;  // of part - from + 1 sums
+  const int q0 = from + warp * each, q1 = min(q0 + each, part + 1);
+  float sum[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+#pragma unroll 4
+  for (int q = q0; q < q1; ++q) {
+    const float *s = (q == part ? w.head : w.tail) + ((int64_t)q * w.slabs + slab) * kSlab;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = s[e * 32 + lane];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += v[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[warp][e * 32 + lane] = sum[e];
+  __syncthreads();
+  const int col = slab * kSlab + threadIdx.x;
   if (col >= w.dim) return;
-  float sum = 0.f;
-#pragma unroll 8
-  for (int64_t q = from; q < part; ++q) sum += w.tail[(q * w.slabs + slab) * kSlab + threadIdx.x];
-  sum += w.head[(part * w.slabs + slab) * kSlab + threadIdx.x];
+  float all = 0.f;
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) all += sums[k][threadIdx.x];
   TD *to = dst + row * w.ldd + col;
   float v[1] = {0.f};
   if (ACC) load_vec<TD, 1>(to, v);
-  v[0] = ACC ? fmaf(w.scale, sum, v[0]) : w.scale * sum;
+  v[0] = ACC ? fmaf(w.scale, all, v[0]) : w.scale * all;
   store_vec<TD, 1>(to, v);
 }
+static_assert(kWalkThreads == kSlab, "a thread per column of the slab");
 
 // ----------------------------------------------------------------------------- dispatch ---
 // Elements per access: the widest of 8, 4, 2, 1 that divides the rows and that both tensors' rows are
-// aligned to (16 bytes at most).
+// aligned to.
 int vector_width(int64_t dim, const void *a, int64_t lda, int32_t ta, const void *b, int64_t ldb, int32_t tb) {
   for (int v = 8; v > 1; v /= 2) {
     auto fits = [&](const void *p, int64_t ld, int32_t t) {
-      const int64_t bytes = std::min<int64_t>(16, (int64_t)v * element_bytes(t));
+      const int64_t bytes = (int64_t)v * element_bytes(t);
       return aligned_to(p, bytes) && ld * element_bytes(t) % bytes == 0;
     };
     if (dim % v == 0 && fits(a, lda, ta) && fits(b, ldb, tb)) return v;
@@ -389,7 +577,7 @@ dion_status dion_embed_plan_create(int64_t vocab, int64_t dim, int64_t max_token
     return DION_ERR_CUDA;
   }
   // one wave of the walk at 4 blocks per SM
-  p->max_parts = std::max<int64_t>(1, (int64_t)p->num_sms * 4 * (kWalkThreads / 32) / p->slabs);
+  p->max_parts = std::max<int64_t>(1, (int64_t)p->num_sms * WB * (kWalkThreads / 32) / p->slabs);
   const int64_t tiles = (max_tokens + kSortTile - 1) / kSortTile;
   size_t off = 0;
   auto region = [&](size_t bytes) {
@@ -463,28 +651,50 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
   int bits = 1;
   while (((int64_t)1 << bits) <= p->vocab) ++bits;
   const int passes = (bits + 8) / 9, digit = (bits + passes - 1) / passes;
-  const int tiles = (int)((num_tokens + kSortTile - 1) / kSortTile);
   int at = 0;
-  for (int pass = 0; pass < passes && tiles > 0 && e == cudaSuccess; ++pass) {
-    const uint32_t *key = pass ? p->key[at] : nullptr, *pos = pass ? p->pos[at] : nullptr;
-    const int shift = pass * digit, next = 1 - at;
-    e = launch(sort_count_kernel, tiles, kSortThreads, 0, s, 1, key, tokens, token_dtype, p->vocab, num_tokens, shift, digit,
-               p->hist);
-    if (e == cudaSuccess)
-      e = launch(sort_move_kernel, tiles, kSortThreads, 0, s, 1, key, pos, tokens, token_dtype, p->vocab, num_tokens, shift,
-                 digit, p->hist, tiles, p->key[next], p->pos[next]);
-    at = next;
+  if (num_tokens > 0 && num_tokens <= (int64_t)kMaxClusterBlocks * kClusterThreads * kMaxClusterItems) {
+    const int64_t rounds = (num_tokens + kClusterThreads - 1) / kClusterThreads;
+    const int blocks = rounds <= C1 ? 1 : kMaxClusterBlocks;
+    const int64_t items = (rounds + blocks - 1) / blocks;
+    auto sort = [&](auto i) {
+      constexpr int I = decltype(i)::value;
+      const size_t smem = kClusterCounts + sizeof(uint2) * kClusterThreads * I;
+      const cudaError_t r = allow_dynamic_smem(sort_cluster_kernel<I>, smem);
+      return r != cudaSuccess ? r
+                              : launch(sort_cluster_kernel<I>, blocks, kClusterThreads, smem, s, blocks, tokens, token_dtype,
+                                       p->vocab, (int32_t)num_tokens, passes, digit, blocks, p->key[0], p->pos[0]);
+    };
+    e = items <= 1   ? sort(std::integral_constant<int, 1>())
+        : items <= 2 ? sort(std::integral_constant<int, 2>())
+        : items <= 4 ? sort(std::integral_constant<int, 4>())
+        : items <= 8 ? sort(std::integral_constant<int, 8>())
+                     : sort(std::integral_constant<int, kMaxClusterItems>());
+  } else {
+    const int tiles = (int)((num_tokens + kSortTile - 1) / kSortTile);
+    for (int pass = 0; pass < passes && tiles > 0 && e == cudaSuccess; ++pass) {
+      const uint32_t *key = pass ? p->key[at] : nullptr, *pos = pass ? p->pos[at] : nullptr;
+      const int shift = pass * digit, next = 1 - at;
+      e = launch(sort_count_kernel, tiles, kSortThreads, 0, s, 1, key, tokens, token_dtype, p->vocab, num_tokens, shift, digit,
+                 p->hist);
+      if (e == cudaSuccess)
+        e = launch(sort_move_kernel, tiles, kSortThreads, 0, s, 1, key, pos, tokens, token_dtype, p->vocab, num_tokens, shift,
+                   digit, p->hist, tiles, p->key[next], p->pos[next]);
+      at = next;
+    }
   }
   if (e != cudaSuccess) return DION_ERR_CUDA;
 
   Walk w{};
   w.key = p->key[at], w.pos = p->pos[at];
-  w.n = num_tokens, w.vocab = p->vocab, w.dim = p->dim, w.ldg = ldg, w.ldd = ldd, w.slabs = p->slabs, w.scale = scale;
+  w.n = (int32_t)num_tokens, w.vocab = (int32_t)p->vocab, w.dim = (int32_t)p->dim, w.slabs = (int32_t)p->slabs;
+  w.ldg = ldg, w.ldd = ldd, w.scale = scale;
   w.head = p->head, w.tail = p->tail, w.head_row = p->head_row, w.tail_row = p->tail_row;
-  const int64_t items = num_tokens + (accumulate ? 0 : p->vocab);
-  w.share = std::max<int64_t>(8, (items + p->max_parts - 1) / p->max_parts);
-  w.parts = (items + w.share - 1) / w.share;
-  const int64_t blocks = (w.parts * w.slabs + kWalkThreads / 32 - 1) / (kWalkThreads / 32);
+  // a row's end writes a row, an entry reads one
+  w.row_cost = RC ? RC : table_grad_dtype == DION_DTYPE_FP32 && grad_dtype == DION_DTYPE_BF16 ? 2 : 1;
+  const int64_t units = num_tokens + (accumulate ? 0 : p->vocab * w.row_cost);
+  w.share = std::max<int64_t>(32, (units + p->max_parts - 1) / p->max_parts);
+  w.parts = (int32_t)((units + w.share - 1) / w.share);
+  const int64_t blocks = ((int64_t)w.parts * w.slabs + kWalkThreads / 32 - 1) / (kWalkThreads / 32);
   const int width = vector_width(p->dim, grad, ldg, grad_dtype, table_grad, ldd, table_grad_dtype);
   e = with_types(grad_dtype, table_grad_dtype, [&](auto tg, auto td) {
     using TG = decltype(tg);
@@ -497,8 +707,8 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
                         : launch(walk_kernel<TG, TD, V, false>, blocks, kWalkThreads, 0, s, 1, w, g, d);
     });
     if (r != cudaSuccess) return r;
-    return accumulate ? launch(join_kernel<TD, true>, w.parts * w.slabs, kSlab, 0, s, 1, w, d)
-                      : launch(join_kernel<TD, false>, w.parts * w.slabs, kSlab, 0, s, 1, w, d);
+    return accumulate ? launch(join_kernel<TD, true>, (int64_t)w.parts * w.slabs, kWalkThreads, 0, s, 1, w, d)
+                      : launch(join_kernel<TD, false>, (int64_t)w.parts * w.slabs, kWalkThreads, 0, s, 1, w, d);
   });
   return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
 }

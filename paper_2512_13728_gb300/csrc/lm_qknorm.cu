@@ -71,30 +71,6 @@ struct Args {
   uint32_t *finished;
 };
 
-// V elements as they sit in memory.
-template <class T, int V>
-struct Raw {
-  static constexpr int kBytes = V * (int)sizeof(T);
-  uint32_t w[kBytes >= 4 ? kBytes / 4 : 1];
-  __device__ __forceinline__ void load(const T *p) {
-    if constexpr (kBytes == 16) {
-      const uint4 x = *reinterpret_cast<const uint4 *>(p);
-      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-    } else if constexpr (kBytes == 8) {
-      const uint2 x = *reinterpret_cast<const uint2 *>(p);
-      w[0] = x.x, w[1] = x.y;
-    } else if constexpr (kBytes == 4) {
-      w[0] = *reinterpret_cast<const uint32_t *>(p);
-    } else {
-      w[0] = *reinterpret_cast<const uint16_t *>(p);
-    }
-  }
-  __device__ __forceinline__ float at(int e) const {
-    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
-    return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-  }
-};
-
 // Where pair u of a head sits: its first element, and the distance to the second.  Pairs at and beyond
 // `half` are the elements that pass.
 template <bool INTER>
@@ -198,7 +174,13 @@ __device__ __forceinline__ void read_pairs(const float *from, int in_group, cons
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
     const int u = (in_group + n * A.group) * V;
-    load_vec<float, V>(from + (2 * u < A.dim ? u : 0), v[n]);
+    const float *at = from + (2 * u < A.dim ? u : 0);
+    if constexpr (V == 8) {  // two accesses: shared memory has none of 32 bytes
+      const float4 x = *reinterpret_cast<const float4 *>(at), y = *reinterpret_cast<const float4 *>(at + 4);
+      v[n][0] = x.x, v[n][1] = x.y, v[n][2] = x.z, v[n][3] = x.w, v[n][4] = y.x, v[n][5] = y.y, v[n][6] = y.z, v[n][7] = y.w;
+    } else {
+      load_vec<float, V>(at, v[n]);
+    }
   }
 }
 
