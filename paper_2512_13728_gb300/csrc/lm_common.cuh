@@ -138,6 +138,13 @@ inline cudaError_t launch(void (*kernel)(P...), int64_t grid, int block, size_t 
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
+// allow_dynamic_smem (three calls of the runtime) where a launch needs it: above 48 KB with the kernels'
+// static shared memory of at most 8 KB.
+template <class... P>
+inline cudaError_t allow_smem(void (*kernel)(P...), size_t smem) {
+  return smem <= 40 * 1024 ? cudaSuccess : allow_dynamic_smem(kernel, smem);
+}
+
 // Makes a plan's device current for the duration of a call.
 struct OnDevice {
   int prev = -1;

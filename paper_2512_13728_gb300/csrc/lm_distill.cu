@@ -704,11 +704,8 @@ dion_status check(const dion_distill *d, float *loss) {
 
 template <class... P>
 cudaError_t run(void (*kernel)(P...), const Args &A, int64_t grid, int threads, size_t smem, cudaStream_t s) {
-  if (smem > 48 * 1024 - kStaticSmem) {
-    const cudaError_t e = allow_dynamic_smem(kernel, smem);
-    if (e != cudaSuccess) return e;
-  }
-  return launch(kernel, grid, threads, smem, s, A.cluster, A);
+  const cudaError_t e = allow_smem(kernel, smem);
+  return e != cudaSuccess ? e : launch(kernel, grid, threads, smem, s, A.cluster, A);
 }
 
 int num_sms() {

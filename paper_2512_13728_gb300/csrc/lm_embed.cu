@@ -4,11 +4,10 @@
 //   gradient  dE[v] (+)= s sum_{i : t_i = v} dy[i]
 //
 // The gradient sorts (token, position) pairs with a stable radix sort (up to 131072 tokens in one
-// cluster of blocks, whose shared memory holds them) and then walks the merge of two lists: the
-// sorted entries and the ends of the table's rows.  Every warp takes an equal share of
-// that merge for a slab of 256 columns, whatever the tokens are: a token that comes thousands of
-// times is split over warps, and the rows that no token names are zeroed along the way.  A row that
-// lies in several shares is added up from the shares' fp32 sums in a second small kernel, in order.
+// cluster of blocks, whose shared memory holds them).  Meanwhile the other SMs zero the rows that no
+// token names.  Then every warp takes an equal share of the sorted entries for a slab of 256 columns,
+// whatever the tokens are: a token that comes thousands of times is split over warps.  A row that lies in
+// several shares is added up from the shares' fp32 sums in a last small kernel, in order.
 #include "lm_common.cuh"
 #include "tc_common.cuh"
 
@@ -28,18 +27,9 @@ constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSlab = 256;        // columns that a warp takes, 8 per lane
 constexpr int kWalkThreads = 256;
-#ifndef WB
-#define WB 4
-#endif
-#ifndef UR
-#define UR 16
-#endif
-#ifndef C1
-#define C1 4
-#endif
-#ifndef RC
-#define RC 0
-#endif
+constexpr int kJoinThreads = 512;
+constexpr int kWalkRegisters = 16;  // of a lane, for rows on their way
+constexpr int kOneBlockRounds = 4;  // of 1024 tokens that one block sorts alone
 
 }  // namespace
 
@@ -47,14 +37,18 @@ struct dion_embed_plan {
   int device = 0, num_sms = 0;
   int64_t vocab = 0, dim = 0, max_tokens = 0;
   void *ws = nullptr;
-  uint32_t *key[2] = {}, *pos[2] = {};  // sorted back and forth
-  uint32_t *hist = nullptr;             // [tiles][kMaxBins]
+  uint2 *entry[2] = {};      // key, position: sorted back and forth
+  uint32_t *hist = nullptr;  // [tiles][kMaxBins]
   float *head = nullptr, *tail = nullptr;  // [max_parts][slabs * kSlab]: sums of rows that begin or end outside a part
   int32_t *head_row = nullptr, *tail_row = nullptr;  // [max_parts]: the rows they belong to, -1: none
   int64_t max_parts = 0, slabs = 0;
 };
 
 namespace {
+
+// The next kernel may start beside this one, which has waited for all before it.  The zeroing kernel does: it
+// needs the tokens alone, and waits for the sort at its end instead of its beginning.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------- lookup ---
 // A warp per token and slab of 256 columns; V elements per access.
@@ -106,8 +100,8 @@ __device__ __forceinline__ uint32_t lanes_with(uint32_t digit, int bits) {
   return same;
 }
 
-// Counts of each digit in each tile of kSortTile entries.  key == null: the first pass, from the tokens.
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t *key, const void *tokens, int32_t dtype,
+// Counts of each digit in each tile of kSortTile entries.  entry == null: the first pass, from the tokens.
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint2 *entry, const void *tokens, int32_t dtype,
                                                                   int64_t vocab, int64_t n, int shift, int bits,
                                                                   uint32_t *hist) {
   __shared__ uint32_t count[kMaxBins];
@@ -118,7 +112,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t
   const int64_t base = (int64_t)blockIdx.x * kSortTile;
   for (int k = threadIdx.x; k < kSortTile; k += kSortThreads) {
     const int64_t i = base + k;
-    if (i < n) atomicAdd(&count[((key ? key[i] : token_key(tokens, dtype, i, vocab)) >> shift) & (bins - 1)], 1u);
+    if (i < n) atomicAdd(&count[((entry ? entry[i].x : token_key(tokens, dtype, i, vocab)) >> shift) & (bins - 1)], 1u);
   }
   __syncthreads();
   for (int b = threadIdx.x; b < bins; b += kSortThreads) hist[(int64_t)blockIdx.x * kMaxBins + b] = count[b];
@@ -127,26 +121,27 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const uint32_t
 // Moves each entry to its place for one digit.  A tile's entries keep their order: warp w holds
 // entries [w 256, (w + 1) 256) in rounds of 32, ranks within a round come from the lanes that share
 // the digit, ranks across rounds and warps from per-warp counters.
-__global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const uint32_t *key, const uint32_t *pos, const void *tokens,
-                                                                 int32_t dtype, int64_t vocab, int64_t n, int shift,
-                                                                 int bits, const uint32_t *hist, int tiles,
-                                                                 uint32_t *key_out, uint32_t *pos_out) {
+__global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const uint2 *entry, const void *tokens, int32_t dtype,
+                                                                 int64_t vocab, int64_t n, int shift,
+                                                                 int bits, const uint32_t *hist, int tiles, int last,
+                                                                 uint2 *out) {
   __shared__ uint32_t first[kMaxBins];              // where this tile's entries of a digit begin
   __shared__ uint32_t count[kSortWarps][kMaxBins];  // of each warp; then where the warp's entries begin
   __shared__ uint32_t warp_total[kSortWarps];
   const int bins = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int b = threadIdx.x; b < kSortWarps * kMaxBins; b += kSortThreads) (&count[0][0])[b] = 0;
   chain_enter();
+  if (last) let_next_start();
   __syncthreads();
-  uint32_t k[kSortItems], p[kSortItems], rank[kSortItems];
+  uint2 held[kSortItems];
+  uint32_t rank[kSortItems];
   const int64_t base = (int64_t)blockIdx.x * kSortTile + warp * (32 * kSortItems) + lane;
 #pragma unroll
   for (int r = 0; r < kSortItems; ++r) {
     const int64_t i = base + r * 32;
     const bool in = i < n;
-    k[r] = in ? (key ? key[i] : token_key(tokens, dtype, i, vocab)) : 0u;
-    p[r] = in ? (pos ? pos[i] : (uint32_t)i) : 0u;
-    const uint32_t digit = in ? (k[r] >> shift) & (bins - 1) : (uint32_t)bins;  // entries past the end match each other only
+    held[r] = !in ? make_uint2(0, 0) : entry ? entry[i] : make_uint2(token_key(tokens, dtype, i, vocab), (uint32_t)i);
+    const uint32_t digit = in ? (held[r].x >> shift) & (bins - 1) : (uint32_t)bins;  // entries past the end match each other only
     const uint32_t same = lanes_with(digit, bits + 1);
     const int leader = __ffs(same) - 1;
     uint32_t before = 0;
@@ -200,11 +195,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const uint32_t 
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kSortItems; ++r) {
-    if (base + r * 32 < n) {
-      const uint32_t at = count[warp][(k[r] >> shift) & (bins - 1)] + rank[r];
-      key_out[at] = k[r];
-      pos_out[at] = p[r];
-    }
+    if (base + r * 32 < n) out[count[warp][(held[r].x >> shift) & (bins - 1)] + rank[r]] = held[r];
   }
 }
 
@@ -229,7 +220,7 @@ __device__ __forceinline__ void store_cluster(uint2 *p, uint32_t rank, uint2 v) 
 template <int I>
 __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const void *tokens, int32_t dtype, int64_t vocab,
                                                                           int32_t n, int passes, int bits, int blocks,
-                                                                          uint32_t *key_out, uint32_t *pos_out) {
+                                                                          uint2 *out) {
   extern __shared__ __align__(16) char sort_mem[];
   uint16_t(*count)[kMaxBins] = reinterpret_cast<uint16_t(*)[kMaxBins]>(sort_mem);  // [warp][digit]
   uint2 *entry = reinterpret_cast<uint2 *>(sort_mem + kClusterCounts);             // [1024 I]: key, position
@@ -239,6 +230,7 @@ __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const 
   constexpr int kHeld = kClusterThreads * I;
   const int begin = warp * 32 * I + lane;  // this lane's first entry in the block
   chain_enter();
+  let_next_start();
   uint32_t k[I], p[I], place[I];
 #pragma unroll
   for (int r = 0; r < I; ++r) {
@@ -276,12 +268,16 @@ __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const 
     }
     if (blocks > 1) {
       tc::cluster_sync();
-      if (tid < bins)
-        for (int b = 0; b < blocks; ++b) {
-          const uint32_t c = load_cluster(&total[pass & 1][tid], b);
-          all += c;
-          if (b < (int)rank) mine += c;
+      if (tid < bins) {
+        uint32_t c[kMaxClusterBlocks];
+#pragma unroll
+        for (int b = 0; b < kMaxClusterBlocks; ++b) c[b] = load_cluster(&total[pass & 1][tid], b);
+#pragma unroll
+        for (int b = 0; b < kMaxClusterBlocks; ++b) {
+          all += c[b];
+          if (b < (int)rank) mine += c[b];
         }
+      }
     } else {
       all = sum;
     }
@@ -311,8 +307,7 @@ __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const 
         else
           entry[at] = make_uint2(k[r], p[r]);
       } else if (at < (uint32_t)n) {
-        key_out[at] = k[r];
-        pos_out[at] = p[r];
+        out[at] = make_uint2(k[r], p[r]);
       }
     }
     if (!last) {
@@ -330,59 +325,62 @@ __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const 
   if (blocks > 1) tc::cluster_sync();  // no block reads the counts of one that is gone
 }
 
+// --------------------------------------------------------------------------------- zero ---
+// Zeros in the rows that no token names.  A block has `rows` rows: it looks through all tokens for them, a
+// flag for each in shared memory, and then writes.  Runs beside the sort.
+constexpr int kZeroThreads = 512, kZeroMaxRows = 8192;
+template <class T>
+__global__ void __launch_bounds__(kZeroThreads) zero_kernel(const void *tokens, int32_t dtype, int32_t n, int32_t vocab, int32_t dim,
+                                                            int32_t rows, T *dst, int64_t ldd, int beside_sort) {
+  __shared__ uint8_t named[kZeroMaxRows];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int first = blockIdx.x * rows, count = min(rows, vocab - first);
+  for (int i = threadIdx.x; i < count; i += kZeroThreads) named[i] = 0;
+  if (!beside_sort) chain_enter();
+  __syncthreads();
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += kZeroThreads) {
+    const int64_t t = load_index(tokens, dtype, i) - first;
+    if (t >= 0 && t < count) named[t] = 1;
+  }
+  __syncthreads();
+  for (int r = warp; r < count; r += kZeroThreads / 32) {
+    if (named[r]) continue;
+    T *row = dst + (int64_t)(first + r) * ldd;
+    const int head = min(dim, (int)((16 - reinterpret_cast<uintptr_t>(row) % 16) % 16 / sizeof(T)));  // up to a multiple of 16 bytes
+    const int chunks = (dim - head) * (int)sizeof(T) / 16, rest = head + chunks * (16 / (int)sizeof(T));
+    if (lane < head) row[lane] = T(0.f);
+    uint4 *to = reinterpret_cast<uint4 *>(row + head);
+    for (int c = lane; c < chunks; c += 32) to[c] = make_uint4(0, 0, 0, 0);
+    if (rest + lane < dim) row[rest + lane] = T(0.f);
+  }
+  if (beside_sort) chain_enter();
+}
+
 // --------------------------------------------------------------------------------- walk ---
 struct Walk {
-  const uint32_t *key, *pos;  // sorted entries
-  int64_t ldg, ldd, share;
-  int32_t n, vocab, dim, parts, slabs;
-  int32_t row_cost;  // of a row's end in the merge, in entries
+  const uint2 *entry;  // sorted: key, position; keys of `vocab` are outside the table, and last
+  int64_t ldg, ldd;
+  int32_t n, vocab, dim, parts, slabs, share;  // part p has the entries [p share, (p + 1) share)
   float scale;
   float *head, *tail;
   int32_t *head_row, *tail_row;
 };
 
-// Entries of the first d units of the merge.  Entry j comes behind j entries and key[j] row ends, so it
-// begins at j + cost key[j]; when accumulating there are no row ends in the merge and it is j.
-// Entries outside the table have places behind the last row end.
-template <bool ACC>
-__device__ __forceinline__ int entries_before(const Walk &w, int64_t d) {
-  if (ACC) return (int)(d < w.n ? d : w.n);
-  const int lane = threadIdx.x & 31;
-  int lo = 0, hi = (int)(w.n < d ? w.n : d);  // the answer lies in [lo, hi]; 33-way search
-  while (hi > lo) {
-    const int step = (hi - lo + 32) / 33;
-    const int j = lo + (lane + 1) * step - 1;  // probe: is entry j among the first d units?
-    const bool in = j < hi && j + (int64_t)w.key[j] * w.row_cost < d;
-    const int hits = __popc(__ballot_sync(0xffffffffu, in));
-    const int h2 = lo + (hits + 1) * step - 1;
-    lo += hits * step;
-    hi = hits < 32 && h2 < hi ? h2 : hi;
-  }
-  return lo;
-}
-
-// One warp: a part of the merge, a slab of columns.
+// One warp: a part of the entries, a slab of columns.  ACC: added to dst instead of written.
 template <class TG, class TD, int V, bool ACC>
 __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_constant__ Walk w, const TG *grad, TD *dst) {
   constexpr int C = 8 / V;
-  constexpr int U = 4 * UR / (C * (int)sizeof(Raw<TG, V>));  // rows loaded together
+  constexpr int U = 4 * kWalkRegisters / (C * (int)sizeof(Raw<TG, V>));  // rows loaded together
   chain_enter();
   const int lane = threadIdx.x & 31;
   const int unit = blockIdx.x * (kWalkThreads / 32) + (threadIdx.x >> 5), part = unit / w.slabs, slab = unit - part * w.slabs;
   if (part >= w.parts) return;
   const int c0 = slab * kSlab + lane * V;
-  const int64_t d0 = part * w.share, d1 = d0 + w.share;
-  int j = entries_before<ACC>(w, d0);
-  const int j1 = entries_before<ACC>(w, d1);
-  // accumulating: the row of the entries at hand, -1 before the first; else the rows that end in this part
-  int row = -1, row_end = 0;
-  if (!ACC) {
-    row = (int)min((d0 - j + w.row_cost - 1) / w.row_cost, (int64_t)w.vocab);
-    row_end = (int)min((d1 - j1 + w.row_cost - 1) / w.row_cost, (int64_t)w.vocab);
-  }
+  const int j0 = part * w.share, j1 = min(j0 + w.share, w.n);
   // the part's first row, where it began in an earlier part: its sums go to the join
-  const int first = ACC ? (j < j1 ? (int)w.key[j] : w.vocab) : row;
-  const int begun = j > 0 && first < w.vocab && (int)w.key[j - 1] == first ? first : -1;
+  const int first = (int)w.entry[j0].x;
+  const int begun = j0 > 0 && first < w.vocab && (int)w.entry[j0 - 1].x == first ? first : -1;
   const int64_t partial = (int64_t)unit * kSlab + lane * V;  // where the part's sums go
   const TG *src = grad + c0;
   TD *out = dst + c0;
@@ -391,10 +389,6 @@ __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_cons
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[c][e] = 0.f;
-  auto put_partial = [&](float *to) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) store_vec<float, V>(to + partial + c * 32 * V, acc[c]);
-  };
   auto end_row = [&](int r) {
     TD *to = out + r * w.ldd;
 #pragma unroll
@@ -412,15 +406,15 @@ __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_cons
       for (int e = 0; e < V; ++e) acc[c][e] = 0.f;
     }
   };
-  int done = j;  // entries of the table so far
-  for (; j < j1; j += 32) {
+  int row = -1, done = j0;  // the row of the entries at hand; entries so far
+  for (int j = j0; j < j1; j += 32) {
     // 32 entries' keys and positions, one per lane
-    const int key = j + lane < j1 ? (int)w.key[j + lane] : w.vocab, pos = j + lane < j1 ? (int)w.pos[j + lane] : 0;
+    const uint2 mine = j + lane < j1 ? w.entry[j + lane] : make_uint2(w.vocab, 0);
     for (int e0 = 0; e0 < 32 && e0 < j1 - j; e0 += U) {
       Raw<TG, V> raw[U][C];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int at = __shfl_sync(0xffffffffu, pos, e0 + u), k = __shfl_sync(0xffffffffu, key, e0 + u);
+        const int at = (int)__shfl_sync(0xffffffffu, mine.y, e0 + u), k = (int)__shfl_sync(0xffffffffu, mine.x, e0 + u);
         const TG *from = src + at * w.ldg;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -431,15 +425,11 @@ __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_cons
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int k = __shfl_sync(0xffffffffu, key, e0 + u);
+        const int k = (int)__shfl_sync(0xffffffffu, mine.x, e0 + u);
         if (k >= w.vocab) break;  // the part's end, or entries outside the table: those come last
         ++done;
-        if (ACC) {
-          if (row >= 0 && row != k) end_row(row);
-          row = k;
-        } else {
-          for (; row < k; ++row) end_row(row);
-        }
+        if (row >= 0 && row != k) end_row(row);
+        row = k;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -448,30 +438,28 @@ __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_cons
     }
   }
   int tail = -1;  // a row that goes on in the next part
-  if (ACC) {
-    if (row >= 0 && done < w.n && (int)w.key[done] == row)
-      tail = row;
-    else if (row >= 0)
-      end_row(row);
-  } else {
-    for (; row < row_end; ++row) end_row(row);
-    if (row < w.vocab && j1 > 0 && (int)w.key[j1 - 1] == row) tail = row;
+  if (row >= 0 && done < w.n && (int)w.entry[done].x == row) {
+    tail = row;
+#pragma unroll
+    for (int c = 0; c < C; ++c) store_vec<float, V>(w.tail + partial + c * 32 * V, acc[c]);
+  } else if (row >= 0) {
+    end_row(row);
   }
-  if (tail >= 0) put_partial(w.tail);
   if (slab == 0 && lane == 0) {
     w.head_row[part] = begun == tail ? -1 : begun;
     w.tail_row[part] = tail;
   }
 }
 
-// Rows that several parts have sums of: a block per part and slab; where the part ends such a row, the
-// warps add up runs of the parts' sums, and the first warp those, in order, and writes the row.
+// Rows that several parts have sums of: a block per part, which has something to do where the part ends
+// such a row.  A warp takes a slab, or with fewer slabs than warps a run of the parts for one; the
+// runs' sums are added in order.
 template <class TD, bool ACC>
-__global__ void __launch_bounds__(kWalkThreads) join_kernel(const __grid_constant__ Walk w, TD *dst) {
-  constexpr int kWarps = kWalkThreads / 32;
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Walk w, TD *dst) {
+  constexpr int kWarps = kJoinThreads / 32;
   __shared__ float sums[kWarps][kSlab];
   chain_enter();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = blockIdx.x / w.slabs, slab = blockIdx.x - part * w.slabs;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = blockIdx.x;
   const int row = w.head_row[part];
   if (row < 0) return;
   int from = part;  // the first of the parts that hold the row, 32 looked at together
@@ -482,35 +470,47 @@ __global__ void __launch_bounds__(kWalkThreads) join_kernel(const __grid_constan
     from -= run;
     more = run == 32;
   }
-  const int each = (part - from + kWarps) / kWarps;  // of part - from + 1 sums
-  const int q0 = from + warp * each, q1 = min(q0 + each, part + 1);
-  float sum[8];
+  const int runs = w.slabs < kWarps ? kWarps / w.slabs : 1;
+  const int each = (part - from + runs) / runs;  // of part - from + 1 sums
+  for (int s0 = 0; s0 < w.slabs; s0 += kWarps / runs) {
+    const int slab = s0 + warp / runs, q0 = from + warp % runs * each, q1 = min(q0 + each, part + 1);
+    float sum[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+    for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+    if (slab < w.slabs && warp < kWarps / runs * runs) {
 #pragma unroll 4
-  for (int q = q0; q < q1; ++q) {
-    const float *s = (q == part ? w.head : w.tail) + ((int64_t)q * w.slabs + slab) * kSlab;
-    float v[8];
+      for (int q = q0; q < q1; ++q) {
+        const float *s = (q == part ? w.head : w.tail) + ((int64_t)q * w.slabs + slab) * kSlab;
+        float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = s[e * 32 + lane];
+        for (int e = 0; e < 8; ++e) v[e] = s[e * 32 + lane];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += v[e];
+        for (int e = 0; e < 8; ++e) sum[e] += v[e];
+      }
+    }
+    if (runs > 1) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sums[warp][e * 32 + lane] = sum[e];
+      __syncthreads();
+      if (warp % runs == 0)
+        for (int k = 1; k < runs; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[e] += sums[(warp + k) % kWarps][e * 32 + lane];
+    }
+    if (slab < w.slabs && warp % runs == 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int col = slab * kSlab + e * 32 + lane;
+        if (col >= w.dim) break;
+        TD *to = dst + row * w.ldd + col;
+        float v[1] = {0.f};
+        if (ACC) load_vec<TD, 1>(to, v);
+        v[0] = ACC ? fmaf(w.scale, sum[e], v[0]) : w.scale * sum[e];
+        store_vec<TD, 1>(to, v);
+      }
+    }
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) sums[warp][e * 32 + lane] = sum[e];
-  __syncthreads();
-  const int col = slab * kSlab + threadIdx.x;
-  if (col >= w.dim) return;
-  float all = 0.f;
-#pragma unroll
-  for (int k = 0; k < kWarps; ++k) all += sums[k][threadIdx.x];
-  TD *to = dst + row * w.ldd + col;
-  float v[1] = {0.f};
-  if (ACC) load_vec<TD, 1>(to, v);
-  v[0] = ACC ? fmaf(w.scale, all, v[0]) : w.scale * all;
-  store_vec<TD, 1>(to, v);
 }
-static_assert(kWalkThreads == kSlab, "a thread per column of the slab");
 
 // ----------------------------------------------------------------------------- dispatch ---
 // Elements per access: the widest of 8, 4, 2, 1 that divides the rows and that both tensors' rows are
@@ -576,8 +576,9 @@ dion_status dion_embed_plan_create(int64_t vocab, int64_t dim, int64_t max_token
     delete p;
     return DION_ERR_CUDA;
   }
-  // one wave of the walk at 4 blocks per SM
-  p->max_parts = std::max<int64_t>(1, (int64_t)p->num_sms * WB * (kWalkThreads / 32) / p->slabs);
+  // one wave of the walk at 4 blocks per SM; no more than 2048 parts, as a token that comes often lies in
+  // many of them and its sums are joined by one block
+  p->max_parts = std::min<int64_t>(2048, std::max<int64_t>(1, (int64_t)p->num_sms * 4 * (kWalkThreads / 32) / p->slabs));
   const int64_t tiles = (max_tokens + kSortTile - 1) / kSortTile;
   size_t off = 0;
   auto region = [&](size_t bytes) {
@@ -585,8 +586,7 @@ dion_status dion_embed_plan_create(int64_t vocab, int64_t dim, int64_t max_token
     off += (bytes + 255) & ~(size_t)255;
     return at;
   };
-  const size_t o_key0 = region(4 * max_tokens), o_key1 = region(4 * max_tokens);
-  const size_t o_pos0 = region(4 * max_tokens), o_pos1 = region(4 * max_tokens);
+  const size_t o_entry0 = region(sizeof(uint2) * max_tokens), o_entry1 = region(sizeof(uint2) * max_tokens);
   const size_t o_hist = region(4 * tiles * kMaxBins);
   const size_t sums = 4 * (size_t)p->max_parts * p->slabs * kSlab;
   const size_t o_head = region(sums), o_tail = region(sums);
@@ -597,8 +597,7 @@ dion_status dion_embed_plan_create(int64_t vocab, int64_t dim, int64_t max_token
     return DION_ERR_CUDA;
   }
   char *b = static_cast<char *>(p->ws);
-  p->key[0] = reinterpret_cast<uint32_t *>(b + o_key0), p->key[1] = reinterpret_cast<uint32_t *>(b + o_key1);
-  p->pos[0] = reinterpret_cast<uint32_t *>(b + o_pos0), p->pos[1] = reinterpret_cast<uint32_t *>(b + o_pos1);
+  p->entry[0] = reinterpret_cast<uint2 *>(b + o_entry0), p->entry[1] = reinterpret_cast<uint2 *>(b + o_entry1);
   p->hist = reinterpret_cast<uint32_t *>(b + o_hist);
   p->head = reinterpret_cast<float *>(b + o_head), p->tail = reinterpret_cast<float *>(b + o_tail);
   p->head_row = reinterpret_cast<int32_t *>(b + o_hrow), p->tail_row = reinterpret_cast<int32_t *>(b + o_trow);
@@ -654,15 +653,15 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
   int at = 0;
   if (num_tokens > 0 && num_tokens <= (int64_t)kMaxClusterBlocks * kClusterThreads * kMaxClusterItems) {
     const int64_t rounds = (num_tokens + kClusterThreads - 1) / kClusterThreads;
-    const int blocks = rounds <= C1 ? 1 : kMaxClusterBlocks;
+    const int blocks = rounds <= kOneBlockRounds ? 1 : kMaxClusterBlocks;
     const int64_t items = (rounds + blocks - 1) / blocks;
     auto sort = [&](auto i) {
       constexpr int I = decltype(i)::value;
       const size_t smem = kClusterCounts + sizeof(uint2) * kClusterThreads * I;
-      const cudaError_t r = allow_dynamic_smem(sort_cluster_kernel<I>, smem);
+      const cudaError_t r = allow_smem(sort_cluster_kernel<I>, smem);
       return r != cudaSuccess ? r
                               : launch(sort_cluster_kernel<I>, blocks, kClusterThreads, smem, s, blocks, tokens, token_dtype,
-                                       p->vocab, (int32_t)num_tokens, passes, digit, blocks, p->key[0], p->pos[0]);
+                                       p->vocab, (int32_t)num_tokens, passes, digit, blocks, p->entry[0]);
     };
     e = items <= 1   ? sort(std::integral_constant<int, 1>())
         : items <= 2 ? sort(std::integral_constant<int, 2>())
@@ -672,28 +671,39 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
   } else {
     const int tiles = (int)((num_tokens + kSortTile - 1) / kSortTile);
     for (int pass = 0; pass < passes && tiles > 0 && e == cudaSuccess; ++pass) {
-      const uint32_t *key = pass ? p->key[at] : nullptr, *pos = pass ? p->pos[at] : nullptr;
+      const uint2 *entry = pass ? p->entry[at] : nullptr;
       const int shift = pass * digit, next = 1 - at;
-      e = launch(sort_count_kernel, tiles, kSortThreads, 0, s, 1, key, tokens, token_dtype, p->vocab, num_tokens, shift, digit,
+      e = launch(sort_count_kernel, tiles, kSortThreads, 0, s, 1, entry, tokens, token_dtype, p->vocab, num_tokens, shift, digit,
                  p->hist);
       if (e == cudaSuccess)
-        e = launch(sort_move_kernel, tiles, kSortThreads, 0, s, 1, key, pos, tokens, token_dtype, p->vocab, num_tokens, shift,
-                   digit, p->hist, tiles, p->key[next], p->pos[next]);
+        e = launch(sort_move_kernel, tiles, kSortThreads, 0, s, 1, entry, tokens, token_dtype, p->vocab, num_tokens, shift,
+                   digit, p->hist, tiles, pass == passes - 1, p->entry[next]);
       at = next;
     }
   }
   if (e != cudaSuccess) return DION_ERR_CUDA;
 
   Walk w{};
-  w.key = p->key[at], w.pos = p->pos[at];
+  w.entry = p->entry[at];
   w.n = (int32_t)num_tokens, w.vocab = (int32_t)p->vocab, w.dim = (int32_t)p->dim, w.slabs = (int32_t)p->slabs;
   w.ldg = ldg, w.ldd = ldd, w.scale = scale;
   w.head = p->head, w.tail = p->tail, w.head_row = p->head_row, w.tail_row = p->tail_row;
-  // a row's end writes a row, an entry reads one
-  w.row_cost = RC ? RC : table_grad_dtype == DION_DTYPE_FP32 && grad_dtype == DION_DTYPE_BF16 ? 2 : 1;
-  const int64_t units = num_tokens + (accumulate ? 0 : p->vocab * w.row_cost);
-  w.share = std::max<int64_t>(32, (units + p->max_parts - 1) / p->max_parts);
-  w.parts = (int32_t)((units + w.share - 1) / w.share);
+  if (!accumulate) {
+    // two blocks on each SM that the sort leaves
+    const int64_t want = 2 * std::max(1, p->num_sms - kMaxClusterBlocks), rows = (p->vocab + want - 1) / want;
+    const int32_t per = (int32_t)std::min<int64_t>(rows, kZeroMaxRows);
+    const int64_t grid = (p->vocab + per - 1) / per;
+    const int beside = num_tokens > 0;
+    e = table_grad_dtype == DION_DTYPE_FP32
+            ? launch(zero_kernel<float>, grid, kZeroThreads, 0, s, 1, tokens, token_dtype, w.n, w.vocab, w.dim, per,
+                     static_cast<float *>(table_grad), ldd, beside)
+            : launch(zero_kernel<__nv_bfloat16>, grid, kZeroThreads, 0, s, 1, tokens, token_dtype, w.n, w.vocab, w.dim, per,
+                     static_cast<__nv_bfloat16 *>(table_grad), ldd, beside);
+    if (e != cudaSuccess) return DION_ERR_CUDA;
+  }
+  if (num_tokens == 0) return DION_OK;
+  w.share = (int32_t)std::max<int64_t>(8, (num_tokens + p->max_parts - 1) / p->max_parts);
+  w.parts = (w.n + w.share - 1) / w.share;
   const int64_t blocks = ((int64_t)w.parts * w.slabs + kWalkThreads / 32 - 1) / (kWalkThreads / 32);
   const int width = vector_width(p->dim, grad, ldg, grad_dtype, table_grad, ldd, table_grad_dtype);
   e = with_types(grad_dtype, table_grad_dtype, [&](auto tg, auto td) {
@@ -707,8 +717,8 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
                         : launch(walk_kernel<TG, TD, V, false>, blocks, kWalkThreads, 0, s, 1, w, g, d);
     });
     if (r != cudaSuccess) return r;
-    return accumulate ? launch(join_kernel<TD, true>, (int64_t)w.parts * w.slabs, kWalkThreads, 0, s, 1, w, d)
-                      : launch(join_kernel<TD, false>, (int64_t)w.parts * w.slabs, kWalkThreads, 0, s, 1, w, d);
+    return accumulate ? launch(join_kernel<TD, true>, w.parts, kJoinThreads, 0, s, 1, w, d)
+                      : launch(join_kernel<TD, false>, w.parts, kJoinThreads, 0, s, 1, w, d);
   });
   return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
 }
