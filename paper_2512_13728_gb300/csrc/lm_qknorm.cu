@@ -6,9 +6,12 @@
 //
 // A group of lanes holds a head as D / 2 pairs (the elements that pass are paired across their own
 // halves, with angle 0), so a rotation never leaves a lane; the mean is a shuffle sum over the group.
-// A warp takes one token at a time: its sines and cosines are computed once by the warp's lanes, and
-// several heads per group are loaded before the first is used.
+// A warp keeps to one kind and a few of its heads and goes over tokens: it computes a token's sines and
+// cosines once, and holds the weights and the sums of their gradients in registers.  What it reads runs
+// ahead of it through a ring of asynchronous copies in shared memory, of which every lane reads only what
+// it copied itself.
 #include "lm_common.cuh"
+#include "tc_common.cuh"
 
 #include <algorithm>
 #include <cmath>
@@ -21,16 +24,13 @@ namespace {
 constexpr int kMaxHeadDim = 256;
 constexpr int kMaxPairs = kMaxHeadDim / 2;
 constexpr int kMaxHeads = 2048;  // of q, of k
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-#ifndef FU
-#define FU 4
-#define FB 1
-#define BU 2
-#define BB 2
-#endif
-constexpr int kForwardHeads = FU;   // heads that a group has in flight
-constexpr int kBackwardHeads = BU;
+constexpr int kRing = 4;      // steps (a head per group of lanes) on their way
+constexpr int kMaxSteps = 8;  // of a token, for a warp
+// Blocks per SM, by the pairs that a lane holds: eight of them take 96 registers forward, 158 backward.
+constexpr int forward_blocks(int pairs) { return pairs == 8 ? 5 : 6; }
+constexpr int backward_blocks(int pairs) { return pairs == 8 ? 3 : 4; }
 }  // namespace
 
 struct dion_qknorm_plan {
@@ -40,8 +40,7 @@ struct dion_qknorm_plan {
   void *ws = nullptr;
   uint64_t *turn = nullptr;     // [rotary / 2]: turns per position as a fraction of 2^64
   float *partial = nullptr;     // [max_blocks][2][head_dim]: a block's sums of dwq, dwk
-  uint32_t *finished = nullptr; // blocks that have written theirs
-  int64_t max_blocks = 0;
+  int64_t max_blocks = 0;       // of the backward kernel
 };
 
 namespace {
@@ -52,11 +51,10 @@ struct Heads {
 };
 
 struct Args {
-  int64_t batch, tokens;  // sequences, tokens of each
-  int64_t tasks;          // forward: tokens of all sequences * parts
+  int32_t tokens, all;  // of a sequence, of all
   int32_t hq, hk;
-  int32_t q_batches, batches;  // batches of heads (one kind each) of q, of q and k
-  int32_t parts;               // warps that share a token's batches
+  int32_t q_steps, k_steps;  // of a token: a head for each group of a warp's lanes
+  int32_t steps;             // of these, what a warp takes (a batch) at most
   int32_t dim, half;           // half = rotary / 2
   int32_t group;               // lanes per head
   float eps;
@@ -66,9 +64,7 @@ struct Args {
   const uint64_t *turn;
   Heads q, k, gq, gk, oq, ok;
   const float *wq, *wk;
-  float *dwq, *dwk;
-  float *partial;
-  uint32_t *finished;
+  float *partial;  // null: no gradient of the weights
 };
 
 // Where pair u of a head sits: its first element, and the distance to the second.  Pairs at and beyond
@@ -84,54 +80,104 @@ __device__ __forceinline__ void pair_place(int u, int dim, int half, int &at, in
   }
 }
 
-// A lane's pairs of a head: NC chunks of V, `group` lanes apart; V divides half and dim / 2 - half unless
-// interleaved, when a chunk's pairs are 2 V neighbouring elements.
+// A lane's pairs of a head are NC chunks of V, `group` lanes apart; V divides half and dim / 2 - half unless
+// interleaved, when a chunk's pairs are 2 V neighbouring elements.  In memory and in the ring a chunk is
+// two pieces of V elements (the pairs' firsts and seconds, or its two halves).
 template <class T, int V, int NC, bool INTER>
-struct HeadPairs {
-  Raw<T, V> lo[NC], hi[NC];
-  __device__ __forceinline__ void load(const T *x, bool on, int in_group, const Args &A) {
+struct Lane {
+  static constexpr int kPairs = NC * V, kPacks = kPairs / 2;
+  static constexpr int kPiece = V * (int)sizeof(T);   // bytes
+  static constexpr int kStep = 2 * NC * 32 * kPiece;  // of a warp's ring, a step of one tensor
+  int at[NC], apart[NC];  // the pieces' first elements in a head: at, at + apart
+  bool has[NC];
+  __device__ __forceinline__ Lane(const Args &A) {
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-      const int u = (in_group + n * A.group) * V;
+      const int u = first_pair(A, n);
+      has[n] = 2 * u < A.dim;
+      at[n] = apart[n] = 0;
+      if (has[n]) pair_place<INTER>(u, A.dim, A.half, at[n], apart[n]);
+      if (INTER) apart[n] = V;
+    }
+  }
+  static __device__ __forceinline__ int first_pair(const Args &A, int n) {
+    return ((threadIdx.x & (A.group - 1)) + n * A.group) * V;
+  }
+  // starts the copies of a head into a step of the ring; zeros where there is no head or chunk
+  __device__ __forceinline__ void copy(const T *x, bool on, char *step) const {
+    char *to = step + (threadIdx.x & 31) * kPiece;
 #pragma unroll
-      for (uint32_t &w : lo[n].w) w = 0;
+    for (int n = 0; n < NC; ++n) {
+      const bool real = on && has[n];
 #pragma unroll
-      for (uint32_t &w : hi[n].w) w = 0;
-      if (on && 2 * u < A.dim) {
-        int at, apart;
-        pair_place<INTER>(u, A.dim, A.half, at, apart);
-        lo[n].load(x + at);
-        hi[n].load(x + at + (INTER ? V : apart));
+      for (int h = 0; h < 2; ++h, to += 32 * kPiece) {
+        const T *from = x + at[n] + h * apart[n];
+        if constexpr (kPiece == 16)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(to)), "l"(from), "r"(real ? 16 : 0) : "memory");
+        else if constexpr (kPiece >= 4)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(tc::smem_u32(to)), "l"(from), "n"(kPiece),
+                       "r"(real ? kPiece : 0)
+                       : "memory");
+        else
+          *reinterpret_cast<T *>(to) = real ? *from : T(0.f);
       }
     }
   }
-  __device__ __forceinline__ float a(int n, int e) const {
-    if (!INTER) return lo[n].at(e);
-    return 2 * e < V ? lo[n].at((2 * e) % V) : hi[n].at((2 * e) % V);
+  // a step's pairs, packed in twos: firsts and seconds
+  __device__ __forceinline__ void read(const char *step, uint64_t (&a)[kPacks], uint64_t (&b)[kPacks]) const {
+    const char *from = step + (threadIdx.x & 31) * kPiece;
+    float x[2][kPairs];
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        Raw<T, V> raw;
+        raw.load(reinterpret_cast<const T *>(from + (2 * n + h) * 32 * kPiece));
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (INTER)  // element h V + e of the chunk's 2 V
+            x[(h * V + e) & 1][n * V + (h * V + e) / 2] = raw.at(e);
+          else
+            x[h][n * V + e] = raw.at(e);
+        }
+      }
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) a[i] = pack2(x[0][2 * i], x[0][2 * i + 1]), b[i] = pack2(x[1][2 * i], x[1][2 * i + 1]);
   }
-  __device__ __forceinline__ float b(int n, int e) const {
-    if (!INTER) return hi[n].at(e);
-    return 2 * e + 1 < V ? lo[n].at((2 * e + 1) % V) : hi[n].at((2 * e + 1) % V);
+  __device__ __forceinline__ void store(T *y, const uint64_t (&a)[kPacks], const uint64_t (&b)[kPacks]) const {
+    float x[2][kPairs];
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) unpack2(a[i], x[0][2 * i], x[0][2 * i + 1]), unpack2(b[i], x[1][2 * i], x[1][2 * i + 1]);
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      if (!has[n]) continue;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = INTER ? x[(h * V + e) & 1][n * V + (h * V + e) / 2] : x[h][n * V + e];
+        store_vec<T, V>(y + at[n] + h * apart[n], v);
+      }
+    }
+  }
+  // the lane's values of an array of pairs in shared memory
+  __device__ __forceinline__ void read_pairs(const float *from, const Args &A, uint64_t (&v)[kPacks]) const {
+    float x[kPairs];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const float *p = from + (has[n] ? first_pair(A, n) : 0);
+#pragma unroll
+      for (int e = 0; e < V; e += V < 4 ? V : 4) {
+        float y[V < 4 ? V : 4];
+        load_vec<float, (V < 4 ? V : 4)>(p + e, y);
+#pragma unroll
+        for (int k = 0; k < (V < 4 ? V : 4); ++k) x[n * V + e + k] = y[k];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) v[i] = pack2(x[2 * i], x[2 * i + 1]);
   }
 };
-template <class T, int V, bool INTER>
-__device__ __forceinline__ void store_pairs(T *x, int u, const Args &A, const float (&a)[V], const float (&b)[V]) {
-  int at, apart;
-  pair_place<INTER>(u, A.dim, A.half, at, apart);
-  if (INTER) {
-    float lo[V], hi[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      lo[e] = e & 1 ? b[e / 2] : a[e / 2];
-      hi[e] = (V + e) & 1 ? b[(V + e) / 2] : a[(V + e) / 2];
-    }
-    store_vec<T, V>(x + at, lo);
-    store_vec<T, V>(x + at + V, hi);
-  } else {
-    store_vec<T, V>(x + at, a);
-    store_vec<T, V>(x + at + apart, b);
-  }
-}
 
 // Sum over the lanes of a group (a power of two, aligned).
 __device__ __forceinline__ float group_sum(float v, int group) {
@@ -168,215 +214,296 @@ __device__ __forceinline__ void stage_weights(const Args &A, float (&w)[2][2][kM
   __syncthreads();
 }
 
-// V neighbouring floats of shared memory for each of a lane's chunks.
-template <int V, int NC>
-__device__ __forceinline__ void read_pairs(const float *from, int in_group, const Args &A, float (&v)[NC][V]) {
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    const int u = (in_group + n * A.group) * V;
-    const float *at = from + (2 * u < A.dim ? u : 0);
-    if constexpr (V == 8) {  // two accesses: shared memory has none of 32 bytes
-      const float4 x = *reinterpret_cast<const float4 *>(at), y = *reinterpret_cast<const float4 *>(at + 4);
-      v[n][0] = x.x, v[n][1] = x.y, v[n][2] = x.z, v[n][3] = x.w, v[n][4] = y.x, v[n][5] = y.y, v[n][6] = y.z, v[n][7] = y.w;
-    } else {
-      load_vec<float, V>(at, v[n]);
-    }
-  }
-}
-
-struct Token {
-  int64_t b, t;
-  __device__ __forceinline__ Token(const Args &A, int64_t i) {
-    if (i <= 0x7fffffff && A.tokens <= 0x7fffffff) {  // a 64-bit division costs more than a head
-      b = (uint32_t)i / (uint32_t)A.tokens;
-    } else {
-      b = i / A.tokens;
-    }
-    t = i - b * A.tokens;
-  }
-  __device__ __forceinline__ int64_t position(const Args &A) const {
-    return A.pos ? load_index(A.pos, A.pos_dtype, b * A.pos_sb + t) : t;
-  }
-  template <class T>
-  __device__ __forceinline__ T *heads(const Heads &H) const {
-    return static_cast<T *>(H.p) + b * H.sb + t * H.st;
+// What a warp goes over: a batch of one kind's heads, and every stride-th token.  A batch of n steps has n
+// of every q_steps + k_steps warps, so that all have the same work.
+struct Unit {
+  int kind, first_head, steps, heads, token, stride;
+  __device__ __forceinline__ Unit(const Args &A, int id) {
+    const int cycle = A.q_steps + A.k_steps, slot = id % cycle;
+    kind = slot >= A.q_steps;
+    heads = kind ? A.hk : A.hq;
+    const int begin = kind ? A.q_steps : 0, in_kind = slot - begin, first_step = in_kind / A.steps * A.steps;
+    first_head = first_step * (32 / A.group);
+    steps = min(A.steps, (kind ? A.k_steps : A.q_steps) - first_step);
+    token = id / cycle * steps + in_kind - first_step;
+    const int warps = (int)gridDim.x * kWarps, left = warps % cycle - (begin + first_step);
+    stride = warps / cycle * steps + max(0, min(left, steps));
   }
 };
 
+// A token and a step of it; runs ahead of the work (the copies) or with it.
+struct Cursor {
+  int token, step, seq, t;  // seq: tokens so far
+  int b;
+  __device__ __forceinline__ Cursor(const Args &A, const Unit &U) : token(U.token), step(0), seq(0) { place(A); }
+  __device__ __forceinline__ void place(const Args &A) {
+    b = (int)((unsigned)token / (unsigned)A.tokens);
+    t = token - b * A.tokens;
+  }
+  __device__ __forceinline__ bool on(const Args &A) const { return token < A.all; }
+  // true where a new token begins
+  __device__ __forceinline__ bool next(const Args &A, const Unit &U) {
+    if (++step < U.steps) return false;
+    step = 0, ++seq;
+    token = U.stride < A.all - token ? token + U.stride : A.all;
+    if (token < A.all) place(A);
+    return true;
+  }
+  template <class T>
+  __device__ __forceinline__ T *head(const Heads &H, int h) const {
+    return static_cast<T *>(H.p) + b * H.sb + t * H.st + h * H.sh;
+  }
+};
+
+// The positions of the tokens on their way: lane 0 copies a token's with its first step.
+template <int S>
+struct Positions {
+  int64_t slot[S];
+  __device__ __forceinline__ void copy(const Args &A, const Cursor &c) {
+    if (!A.pos || c.step != 0 || (threadIdx.x & 31) != 0) return;
+    int64_t *to = &slot[c.seq % S];
+    const int64_t i = (int64_t)c.b * A.pos_sb + c.t;
+    if (A.pos_dtype == DION_INDEX_INT64)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(tc::smem_u32(to)), "l"(static_cast<const int64_t *>(A.pos) + i)
+                   : "memory");
+    else
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::smem_u32(to)), "l"(static_cast<const int32_t *>(A.pos) + i)
+                   : "memory");
+  }
+  // after the copies are complete for lane 0, and a __syncwarp
+  __device__ __forceinline__ int64_t of(const Args &A, const Cursor &c) const {
+    const int64_t *from = &slot[c.seq % S];
+    return !A.pos ? c.t : A.pos_dtype == DION_INDEX_INT64 ? *from : (int64_t)*reinterpret_cast<const int32_t *>(from);
+  }
+};
+
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // ------------------------------------------------------------------------------ forward ---
 template <class T, int V, int NC, bool INTER>
-__global__ void __launch_bounds__(kThreads, FB) forward_kernel(const __grid_constant__ Args A) {
-  constexpr int U = kForwardHeads;
+__global__ void __launch_bounds__(kThreads, forward_blocks(NC * V)) forward_kernel(const __grid_constant__ Args A) {
+  using L = Lane<T, V, NC, INTER>;
+  constexpr int S = kRing, P = L::kPacks;
   __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs];
+  __shared__ __align__(16) char ring[kWarps][S][L::kStep];
+  __shared__ Positions<S> positions[kWarps];
   chain_enter();
-  stage_weights<INTER>(A, w);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_group = lane & (A.group - 1), groups = 32 / A.group;
-  const int64_t task = (int64_t)blockIdx.x * kWarps + warp;
-  if (task >= A.tasks) return;
-  const int64_t i = task <= 0x7fffffff ? (int64_t)((uint32_t)task / (uint32_t)A.parts) : task / A.parts;
-  const Token tok(A, i);
-  const int64_t position = tok.position(A);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = 32 / A.group;
+  const Unit U(A, blockIdx.x * kWarps + warp);
+  const Heads &X = U.kind ? A.k : A.q, &Y = U.kind ? A.ok : A.oq;
+  const L mine(A);
+  const int h0 = U.first_head + lane / A.group;
+  const int64_t x_step = groups * X.sh, y_step = groups * Y.sh;
+  Cursor ahead(A, U), at(A, U);
+  const T *from = ahead.head<const T>(X, h0);
+  T *to = at.head<T>(Y, h0);
+  int filled = 0, used = 0;  // places of the ring
+  auto fill = [&] {
+    if (ahead.on(A)) {
+      mine.copy(from, h0 + ahead.step * groups < U.heads, ring[warp][filled]);
+      positions[warp].copy(A, ahead);
+      if (ahead.next(A, U))
+        from = ahead.head<const T>(X, h0);
+      else
+        from += x_step;
+    }
+    commit_copies();
+    filled = filled + 1 == S ? 0 : filled + 1;
+  };
+#pragma unroll
+  for (int k = 0; k < S - 1; ++k) fill();
+  stage_weights<INTER>(A, w);  // while the first steps are on their way
   const float inv_dim = 1.f / (float)A.dim;
-  bool angles_ready = false;
-  for (int batch = (int)(task - i * A.parts); batch < A.batches; batch += A.parts) {
-    const int kind = batch >= A.q_batches;
-    const int heads = kind ? A.hk : A.hq, h0 = (batch - (kind ? A.q_batches : 0)) * U * groups + lane / A.group;
-    const Heads &X = kind ? A.k : A.q, &Y = kind ? A.ok : A.oq;
-    const T *x = tok.heads<const T>(X);
-    T *y = tok.heads<T>(Y);
-    HeadPairs<T, V, NC, INTER> p[U];
+  uint64_t ac[P], bs[P], bc[P], as[P];  // of a token: wa cos, -wb sin, wb cos, wa sin
+  while (at.on(A)) {
+    wait_copies<S - 2>();
+    if (at.step == 0) {
+      __syncwarp();
+      token_angles(A, positions[warp].of(A, at), angles[warp][0], angles[warp][1]);
+      uint64_t c[P], s[P], wa[P], wb[P];
+      mine.read_pairs(angles[warp][0], A, c);
+      mine.read_pairs(angles[warp][1], A, s);
+      mine.read_pairs(w[U.kind][0], A, wa);
+      mine.read_pairs(w[U.kind][1], A, wb);
 #pragma unroll
-    for (int k = 0; k < U; ++k) p[k].load(x + (h0 + k * groups) * X.sh, h0 + k * groups < heads, in_group, A);
-    if (!angles_ready) token_angles(A, position, angles[warp][0], angles[warp][1]);
-    angles_ready = true;
-    float c[NC][V], s[NC][V], wa[NC][V], wb[NC][V];
-    read_pairs<V, NC>(angles[warp][0], in_group, A, c);
-    read_pairs<V, NC>(angles[warp][1], in_group, A, s);
-    read_pairs<V, NC>(w[kind][0], in_group, A, wa);
-    read_pairs<V, NC>(w[kind][1], in_group, A, wb);
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      if ((batch - (kind ? A.q_batches : 0)) * U * groups + k * groups >= heads) break;  // the same for the whole warp
-      float sum = 0.f;
-#pragma unroll
-      for (int n = 0; n < NC; ++n)
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum = fmaf(p[k].a(n, e), p[k].a(n, e), fmaf(p[k].b(n, e), p[k].b(n, e), sum));
-      const float r = rsqrtf(group_sum(sum, A.group) * inv_dim + A.eps);
-      const int h = h0 + k * groups;
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const int u = (in_group + n * A.group) * V;
-        if (h >= heads || 2 * u >= A.dim) continue;
-        float a[V], b[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float ua = p[k].a(n, e) * r * wa[n][e], ub = p[k].b(n, e) * r * wb[n][e];
-          a[e] = ua * c[n][e] - ub * s[n][e];
-          b[e] = ub * c[n][e] + ua * s[n][e];
-        }
-        store_pairs<T, V, INTER>(y + h * Y.sh, u, A, a, b);
+      for (int i = 0; i < P; ++i) {
+        ac[i] = mul2(wa[i], c[i]), as[i] = mul2(wa[i], s[i]), bc[i] = mul2(wb[i], c[i]);
+        bs[i] = mul2(mul2(wb[i], s[i]), pack2(-1.f, -1.f));
       }
     }
+    uint64_t a[P], b[P], sum2 = 0, sum2b = 0;
+    mine.read(ring[warp][used], a, b);
+    used = used + 1 == S ? 0 : used + 1;
+#pragma unroll
+    for (int i = 0; i < P; ++i) sum2 = fma2(a[i], a[i], sum2), sum2b = fma2(b[i], b[i], sum2b);
+    float sum, more;
+    unpack2(add2(sum2, sum2b), sum, more);
+    const float r = rsqrtf(group_sum(sum + more, A.group) * inv_dim + A.eps);
+    const uint64_t r2 = pack2(r, r);
+    if (h0 + at.step * groups < U.heads) {
+      uint64_t ya[P], yb[P];
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        ya[i] = mul2(r2, fma2(b[i], bs[i], mul2(a[i], ac[i])));
+        yb[i] = mul2(r2, fma2(a[i], as[i], mul2(b[i], bc[i])));
+      }
+      mine.store(to, ya, yb);
+    }
+    if (at.next(A, U))
+      to = at.head<T>(Y, h0);
+    else
+      to += y_step;
+    fill();
   }
 }
 
 // ----------------------------------------------------------------------------- backward ---
-// A warp keeps to one batch of heads and goes over tokens, so that its sums of dw stay in registers.
 template <class T, int V, int NC, bool INTER>
-__global__ void __launch_bounds__(kThreads, BB) backward_kernel(const __grid_constant__ Args A) {
-  constexpr int U = kBackwardHeads;
-  __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs], red[kWarps][2 * kMaxHeadDim];
-  __shared__ bool last;
+__global__ void __launch_bounds__(kThreads, backward_blocks(NC * V)) backward_kernel(const __grid_constant__ Args A) {
+  using L = Lane<T, V, NC, INTER>;
+  constexpr int S = kRing, P = L::kPacks;
+  __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs];
+  __shared__ __align__(16) char ring[kWarps][S][2][L::kStep];
+  __shared__ Positions<S> positions[kWarps];
   chain_enter();
-  stage_weights<INTER>(A, w);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_group = lane & (A.group - 1), groups = 32 / A.group;
-  const int64_t all = A.batch * A.tokens;
-  const int unit = blockIdx.x * kWarps + warp, batch = unit % A.batches;
-  const int64_t first = unit / A.batches, stride = ((int64_t)gridDim.x * kWarps - batch + A.batches - 1) / A.batches;
-  const int kind = batch >= A.q_batches;
-  const int heads = kind ? A.hk : A.hq, h_first = (batch - (kind ? A.q_batches : 0)) * U * groups, h0 = h_first + lane / A.group;
-  const Heads &X = kind ? A.k : A.q, &G = kind ? A.gk : A.gq, &Y = kind ? A.ok : A.oq;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = 32 / A.group;
+  const Unit U(A, blockIdx.x * kWarps + warp);
+  const Heads &X = U.kind ? A.k : A.q, &G = U.kind ? A.gk : A.gq, &Y = U.kind ? A.ok : A.oq;
+  const L mine(A);
+  const int h0 = U.first_head + lane / A.group;
+  const int64_t x_step = groups * X.sh, g_step = groups * G.sh, y_step = groups * Y.sh;
+  Cursor ahead(A, U), at(A, U);
+  const T *from = ahead.head<const T>(X, h0), *from_g = ahead.head<const T>(G, h0);
+  T *to = at.head<T>(Y, h0);
+  int filled = 0, used = 0;
+  auto fill = [&] {
+    if (ahead.on(A)) {
+      const bool on = h0 + ahead.step * groups < U.heads;
+      mine.copy(from, on, ring[warp][filled][0]);
+      mine.copy(from_g, on, ring[warp][filled][1]);
+      positions[warp].copy(A, ahead);
+      if (ahead.next(A, U))
+        from = ahead.head<const T>(X, h0), from_g = ahead.head<const T>(G, h0);
+      else
+        from += x_step, from_g += g_step;
+    }
+    commit_copies();
+    filled = filled + 1 == S ? 0 : filled + 1;
+  };
+#pragma unroll
+  for (int k = 0; k < S - 1; ++k) fill();
+  stage_weights<INTER>(A, w);  // while the first steps are on their way
   const float inv_dim = 1.f / (float)A.dim;
-  float wa[NC][V], wb[NC][V], da[NC][V], db[NC][V];  // weights, and this lane's sums of their gradients
-  read_pairs<V, NC>(w[kind][0], in_group, A, wa);
-  read_pairs<V, NC>(w[kind][1], in_group, A, wb);
+  uint64_t c[P], s[P], ns[P], wa[P], wb[P], da[P], db[P];  // ns = -s; da, db: this lane's sums of dw
+  mine.read_pairs(w[U.kind][0], A, wa);
+  mine.read_pairs(w[U.kind][1], A, wb);
 #pragma unroll
-  for (int n = 0; n < NC; ++n)
+  for (int i = 0; i < P; ++i) da[i] = db[i] = 0;
+  while (at.on(A)) {
+    wait_copies<S - 2>();
+    if (at.step == 0) {
+      __syncwarp();
+      token_angles(A, positions[warp].of(A, at), angles[warp][0], angles[warp][1]);
+      mine.read_pairs(angles[warp][0], A, c);
+      mine.read_pairs(angles[warp][1], A, s);
 #pragma unroll
-    for (int e = 0; e < V; ++e) da[n][e] = db[n][e] = 0.f;
-  for (int64_t i = first; i < all; i += stride) {
-    const Token tok(A, i);
-    const T *x = tok.heads<const T>(X), *g = tok.heads<const T>(G);
-    T *y = tok.heads<T>(Y);
-    HeadPairs<T, V, NC, INTER> p[U], q[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const bool on = h0 + k * groups < heads;
-      p[k].load(x + (h0 + k * groups) * X.sh, on, in_group, A);
-      q[k].load(g + (h0 + k * groups) * G.sh, on, in_group, A);
+      for (int i = 0; i < P; ++i) ns[i] = mul2(s[i], pack2(-1.f, -1.f));
     }
-    token_angles(A, tok.position(A), angles[warp][0], angles[warp][1]);
-    float c[NC][V], s[NC][V];
-    read_pairs<V, NC>(angles[warp][0], in_group, A, c);
-    read_pairs<V, NC>(angles[warp][1], in_group, A, s);
+    uint64_t a[P], b[P], ga[P], gb[P], sum2 = 0, sum2b = 0, dot2 = 0, dot2b = 0;
+    mine.read(ring[warp][used][0], a, b);
+    mine.read(ring[warp][used][1], ga, gb);
+    used = used + 1 == S ? 0 : used + 1;
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      if (h_first + k * groups >= heads) break;  // the same for the whole warp
-      float ga[NC][V], gb[NC][V], sum = 0.f, dot = 0.f;
+    for (int i = 0; i < P; ++i) {
+      const uint64_t oa = ga[i], ob = gb[i];
+      ga[i] = fma2(ob, s[i], mul2(oa, c[i]));
+      gb[i] = fma2(oa, ns[i], mul2(ob, c[i]));
+      sum2 = fma2(a[i], a[i], sum2), sum2b = fma2(b[i], b[i], sum2b);
+      dot2 = fma2(mul2(ga[i], wa[i]), a[i], dot2), dot2b = fma2(mul2(gb[i], wb[i]), b[i], dot2b);
+    }
+    float sum, dot, more;
+    unpack2(add2(sum2, sum2b), sum, more);
+    sum += more;
+    unpack2(add2(dot2, dot2b), dot, more);
+    dot += more;
+    for (int o = A.group >> 1; o > 0; o >>= 1) {
+      sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    }
+    const float r = rsqrtf(sum * inv_dim + A.eps);
+    const float back = -dot * inv_dim * r * r * r;  // dx = r w gu - x r^3 mean(w gu x)
+    const uint64_t r2 = pack2(r, r), back2 = pack2(back, back);
+    if (h0 + at.step * groups < U.heads) {
 #pragma unroll
-      for (int n = 0; n < NC; ++n)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float a = p[k].a(n, e), b = p[k].b(n, e), oa = q[k].a(n, e), ob = q[k].b(n, e);
-          ga[n][e] = oa * c[n][e] + ob * s[n][e];
-          gb[n][e] = ob * c[n][e] - oa * s[n][e];
-          sum = fmaf(a, a, fmaf(b, b, sum));
-          dot = fmaf(ga[n][e] * wa[n][e], a, fmaf(gb[n][e] * wb[n][e], b, dot));
-        }
-      sum = group_sum(sum, A.group);
-      dot = group_sum(dot, A.group);
-      const float r = rsqrtf(sum * inv_dim + A.eps);
-      const float back = dot * inv_dim * r * r * r;  // dx = r w gu - x r^3 mean(w gu x)
-      const int h = h0 + k * groups;
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const int u = (in_group + n * A.group) * V;
-        if (h >= heads || 2 * u >= A.dim) continue;
-        float oa[V], ob[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float a = p[k].a(n, e), b = p[k].b(n, e), ra = r * ga[n][e], rb = r * gb[n][e];
-          da[n][e] = fmaf(ra, a, da[n][e]), db[n][e] = fmaf(rb, b, db[n][e]);
-          oa[e] = ra * wa[n][e] - a * back;
-          ob[e] = rb * wb[n][e] - b * back;
-        }
-        store_pairs<T, V, INTER>(y + h * Y.sh, u, A, oa, ob);
+      for (int i = 0; i < P; ++i) {
+        const uint64_t ra = mul2(r2, ga[i]), rb = mul2(r2, gb[i]);
+        da[i] = fma2(ra, a[i], da[i]), db[i] = fma2(rb, b[i], db[i]);
+        a[i] = fma2(ra, wa[i], mul2(a[i], back2));
+        b[i] = fma2(rb, wb[i], mul2(b[i], back2));
       }
+      mine.store(to, a, b);
     }
+    if (at.next(A, U))
+      to = at.head<T>(Y, h0);
+    else
+      to += y_step;
+    fill();
   }
-  if (!A.dwq && !A.dwk) return;
-  // the block's sums of dw: over the groups of a warp, then over the warps, then over the blocks, each
-  // in a fixed order; the last block to finish adds up the blocks
-  for (int d = lane; d < 2 * A.dim; d += 32) red[warp][d] = 0.f;
+  if (!A.partial) return;
+  // the block's sums of dw, over the groups of a warp, then over the warps, in the angles' place
+  __syncwarp();
+  float *red = &angles[0][0][0];  // [kWarps][dim] of the warp's kind
+  for (int d = lane; d < A.dim; d += 32) red[warp * 2 * kMaxPairs + d] = 0.f;
   __syncwarp();
 #pragma unroll
-  for (int n = 0; n < NC; ++n)
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      float va = da[n][e], vb = db[n][e];
-      for (int o = A.group; o < 32; o <<= 1) {
-        va += __shfl_xor_sync(0xffffffffu, va, o);
-        vb += __shfl_xor_sync(0xffffffffu, vb, o);
-      }
-      const int u = (in_group + n * A.group) * V + e;
-      if (lane < A.group && 2 * u < A.dim) {
-        int at, apart;
-        pair_place<INTER>(u, A.dim, A.half, at, apart);
-        red[warp][kind * A.dim + at] = va, red[warp][kind * A.dim + at + apart] = vb;
-      }
+  for (int i = 0; i < L::kPairs; ++i) {
+    float v[4];
+    unpack2(da[i / 2], v[0], v[1]);
+    unpack2(db[i / 2], v[2], v[3]);
+    float va = v[i & 1], vb = v[2 + (i & 1)];
+    for (int o = A.group; o < 32; o <<= 1) {
+      va += __shfl_xor_sync(0xffffffffu, va, o);
+      vb += __shfl_xor_sync(0xffffffffu, vb, o);
     }
+    if (lane < A.group && mine.has[i / V]) {
+      int place, apart;
+      pair_place<INTER>(L::first_pair(A, i / V) + i % V, A.dim, A.half, place, apart);
+      red[warp * 2 * kMaxPairs + place] = va, red[warp * 2 * kMaxPairs + place + apart] = vb;
+    }
+  }
   __syncthreads();
   for (int d = threadIdx.x; d < 2 * A.dim; d += kThreads) {
+    const int kind = d >= A.dim;
     float v = 0.f;
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) v += red[k][d];
+    for (int k = 0; k < kWarps; ++k)
+      if ((((int)blockIdx.x * kWarps + k) % (A.q_steps + A.k_steps) >= A.q_steps) == (kind != 0)) v += red[k * 2 * kMaxPairs + d - kind * A.dim];
     A.partial[(int64_t)blockIdx.x * 2 * A.dim + d] = v;
   }
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(A.finished, 1u) == gridDim.x - 1;
-  __syncthreads();
-  if (!last) return;
-  __threadfence();
-  for (int d = threadIdx.x; d < 2 * A.dim; d += kThreads) {
-    float v = 0.f;
+}
+
+// dw from the blocks' sums: a block per 32 columns, whose warps take the rows in turn; fixed order.
+constexpr int kSumThreads = 1024;
+__global__ void __launch_bounds__(kSumThreads) sum_weights_kernel(const float *partial, int blocks, int dim, float *dwq, float *dwk) {
+  __shared__ float red[kSumThreads / 32][33];
+  chain_enter();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = blockIdx.x * 32 + lane;
+  float v = 0.f;
+  if (d < 2 * dim)
 #pragma unroll 8
-    for (int blk = 0; blk < (int)gridDim.x; ++blk) v += __ldcg(&A.partial[(int64_t)blk * 2 * A.dim + d]);
-    float *to = d < A.dim ? A.dwq : A.dwk;
-    if (to) to[d < A.dim ? d : d - A.dim] = v;
-  }
-  if (threadIdx.x == 0) *A.finished = 0;  // for the next call
+    for (int b = warp; b < blocks; b += kSumThreads / 32) v += partial[(int64_t)b * 2 * dim + d];
+  red[warp][lane] = v;
+  __syncthreads();
+  v = red[lane][warp];  // lane l: the sum of warp l for column `warp`
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  const int col = blockIdx.x * 32 + warp;
+  if (lane != 0 || col >= 2 * dim) return;
+  float *to = col < dim ? dwq : dwk;
+  if (to) to[col < dim ? col : col - dim] = v;
 }
 
 // ----------------------------------------------------------------------------- dispatch ---
@@ -410,23 +537,29 @@ dion_status check_shape(const dion_qknorm_plan *p, const dion_qk_shape *s) {
   if (s->positions && !is_index(s->position_dtype)) return DION_ERR_INVALID_ARG;
   if (s->heads > kMaxHeads || s->kv_heads > kMaxHeads) return DION_ERR_UNSUPPORTED;
   if (s->positions && !aligned_to(s->positions, s->position_dtype == DION_INDEX_INT64 ? 8 : 4)) return DION_ERR_ALIGNMENT;
+  if (s->batch > 0 && s->tokens > INT32_MAX / s->batch) return DION_ERR_UNSUPPORTED;
   const int64_t limit = (int64_t)1 << 40, per = ((int64_t)s->heads + s->kv_heads) * p->head_dim;
   if (s->batch > 0 && s->tokens > 0 && (per > limit || s->batch > limit / per || s->tokens > limit / per / s->batch))
     return DION_ERR_UNSUPPORTED;
   return DION_OK;
 }
 
-Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int v, int nc, int heads_in_flight) {
+// Args of a call whose kernel has `blocks` resident blocks, and the blocks that it takes.
+Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int v, int nc, int64_t resident, int64_t *blocks) {
   Args A{};
-  A.batch = s->batch, A.tokens = s->tokens, A.hq = s->heads, A.hk = s->kv_heads;
+  A.tokens = (int32_t)s->tokens, A.all = (int32_t)(s->batch * s->tokens);
+  A.hq = s->heads, A.hk = s->kv_heads;
   A.dim = p->head_dim, A.half = p->rotary / 2, A.eps = p->eps;
   A.pos = s->positions, A.pos_sb = s->position_batch_stride, A.pos_dtype = s->position_dtype;
-  A.turn = p->turn, A.partial = p->partial, A.finished = p->finished;
+  A.turn = p->turn;
   A.group = 1;
   while (A.group * nc * v < p->head_dim / 2) A.group *= 2;
-  const int per = heads_in_flight * (32 / A.group);
-  A.q_batches = (int32_t)(((int64_t)A.hq + per - 1) / per);
-  A.batches = A.q_batches + (int32_t)(((int64_t)A.hk + per - 1) / per);
+  const int groups = 32 / A.group;
+  A.q_steps = (A.hq + groups - 1) / groups, A.k_steps = (A.hk + groups - 1) / groups;
+  const int64_t cycle = A.q_steps + A.k_steps, work = A.all * cycle;
+  // a warp takes several steps of a token, which share its angles, as far as every warp has some
+  A.steps = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kMaxSteps, work / (resident * kWarps)));
+  *blocks = (std::max(std::min(resident * kWarps, work), cycle) + kWarps - 1) / kWarps;
   return A;
 }
 
@@ -471,17 +604,15 @@ dion_status dion_qknorm_plan_create(int32_t head_dim, int32_t rotary_dim, int32_
   p->head_dim = head_dim, p->rotary = rotary_dim, p->interleaved = interleaved != 0, p->eps = eps;
   cudaError_t e = cudaGetDevice(&p->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->num_sms, cudaDevAttrMultiProcessorCount, p->device);
-  // two resident blocks per SM, and a warp for every batch of the most heads that a call may have
-  p->max_blocks = std::max<int64_t>(2 * (int64_t)p->num_sms, 2 * kMaxHeads / kBackwardHeads / kWarps);
-  const size_t o_partial = sizeof(turn), o_done = o_partial + sizeof(float) * 2 * head_dim * p->max_blocks;
-  if (e == cudaSuccess) e = cudaMalloc(&p->ws, o_done + 16);
+  // the resident blocks, or a warp for every batch of the most heads that a call may have
+  p->max_blocks = std::max<int64_t>((int64_t)p->num_sms * backward_blocks(4), 2 * kMaxHeads / kWarps);
+  const size_t o_partial = sizeof(turn);
+  if (e == cudaSuccess) e = cudaMalloc(&p->ws, o_partial + sizeof(float) * 2 * head_dim * p->max_blocks);
   if (e == cudaSuccess) {
     char *b = static_cast<char *>(p->ws);
     p->turn = reinterpret_cast<uint64_t *>(b);
     p->partial = reinterpret_cast<float *>(b + o_partial);
-    p->finished = reinterpret_cast<uint32_t *>(b + o_done);
     e = cudaMemcpy(p->turn, turn, sizeof(turn), cudaMemcpyHostToDevice);
-    if (e == cudaSuccess) e = cudaMemset(p->finished, 0, 16);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
   }
   if (e != cudaSuccess) {
@@ -511,14 +642,9 @@ dion_status dion_qknorm_forward(dion_qknorm_plan *p, const dion_qk_shape *s, con
   const Heads h[4] = {heads_of(s->heads ? q : nullptr), heads_of(s->kv_heads ? k : nullptr),
                       heads_of(s->heads ? q_out : nullptr), heads_of(s->kv_heads ? k_out : nullptr)};
   const int v = pair_width(p, s, h, 4);
-  Args A = make_args(p, s, v, chunks_per_lane(v), kForwardHeads);
+  int64_t blocks = 0;
+  Args A = make_args(p, s, v, chunks_per_lane(v), (int64_t)p->num_sms * forward_blocks(chunks_per_lane(v) * v), &blocks);
   A.q = h[0], A.k = h[1], A.oq = h[2], A.ok = h[3], A.wq = wq, A.wk = wk;
-  // a warp per token, or more where the tokens do not give every SM its 16 warps
-  const int64_t all = s->batch * s->tokens;
-  A.parts = (int32_t)std::min<int64_t>(A.batches, ((int64_t)p->num_sms * 16 + all - 1) / all);
-  A.tasks = all * A.parts;
-  const int64_t blocks = (A.tasks + kWarps - 1) / kWarps;
-  if (blocks > INT32_MAX) return DION_ERR_UNSUPPORTED;
   const cudaError_t e = with_kernel(s->dtype, v, p->interleaved, [&](auto t, auto V, auto NC, auto I) {
     return launch(forward_kernel<decltype(t), decltype(V)::value, decltype(NC)::value, decltype(I)::value>, blocks, kThreads,
                   0, static_cast<cudaStream_t>(stream), 1, A);
@@ -549,16 +675,17 @@ dion_status dion_qknorm_backward(dion_qknorm_plan *p, const dion_qk_shape *s, co
     h[i] = heads_of(n ? in[i] : nullptr);
   }
   const int v = pair_width(p, s, h, 6);
-  Args A = make_args(p, s, v, chunks_per_lane(v), kBackwardHeads);
+  int64_t blocks = 0;
+  Args A = make_args(p, s, v, chunks_per_lane(v), (int64_t)p->num_sms * backward_blocks(chunks_per_lane(v) * v), &blocks);
   A.gq = h[0], A.gk = h[1], A.q = h[2], A.k = h[3], A.oq = h[4], A.ok = h[5];
-  A.wq = wq, A.wk = wk, A.dwq = dwq, A.dwk = dwk;
-  const int64_t units = s->batch * s->tokens * A.batches;
-  const int64_t blocks = std::max<int64_t>(std::min(p->max_blocks, (units + kWarps - 1) / kWarps),
-                                           (A.batches + kWarps - 1) / kWarps);  // a warp for every batch of heads
-  const cudaError_t e = with_kernel(s->dtype, v, p->interleaved, [&](auto t, auto V, auto NC, auto I) {
+  A.wq = wq, A.wk = wk, A.partial = dwq || dwk ? p->partial : nullptr;
+  cudaError_t e = with_kernel(s->dtype, v, p->interleaved, [&](auto t, auto V, auto NC, auto I) {
     return launch(backward_kernel<decltype(t), decltype(V)::value, decltype(NC)::value, decltype(I)::value>, blocks, kThreads,
                   0, cs, 1, A);
   });
+  if (e == cudaSuccess && A.partial)
+    e = launch(sum_weights_kernel, (2 * p->head_dim + 31) / 32, kSumThreads, 0, cs, 1, p->partial, (int)blocks, p->head_dim, dwq,
+               dwk);
   return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
 }
 
