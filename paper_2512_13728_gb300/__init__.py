@@ -24,7 +24,8 @@ def __getattr__(name: str):
     if name in _LM:
         from . import lm
 
-        return getattr(lm, name)
+        globals().update((n, getattr(lm, n)) for n in _LM)
+        return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 

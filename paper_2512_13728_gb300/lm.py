@@ -175,6 +175,20 @@ class QKNormPlan:
             raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} on {self.device} with contiguous heads")
         return _HEADS.pack(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
 
+    def _outputs(self, out, qs, ks, dtype):
+        """The outputs of q's and k's shapes (those given, or new ones), each with its packed dion_heads."""
+        if out is not None:
+            oq, ok = out
+            if (ok is None) != (ks is None):
+                raise ValueError("out must have a tensor for k where there is one")
+            return oq, self._heads("out[0]", oq, qs, dtype), ok, self._heads("out[1]", ok, ks, dtype)
+        d = self.head_dim
+        oq, ok, hok = torch.empty(qs, dtype=dtype, device=self.device), None, None
+        if ks is not None:
+            ok = torch.empty(ks, dtype=dtype, device=self.device)
+            hok = _HEADS.pack(ok.data_ptr(), ks[-3] * ks[-2] * d, ks[-2] * d, d)
+        return oq, _HEADS.pack(oq.data_ptr(), qs[-3] * qs[-2] * d, qs[-2] * d, d), ok, hok
+
     def _shape(self, q, k, positions):
         """A packed dion_qk_shape, and the dtype."""
         dims, dtype = q.shape, q.dtype
@@ -209,15 +223,8 @@ class QKNormPlan:
         qs, ks = q.shape, None if k is None else k.shape
         hq, hk = self._heads("q", q, qs, dtype), self._heads("k", k, ks, dtype)
         s = _stream(self._index, stream, out is not None)
-        if out is None:
-            oq = torch.empty(qs, dtype=dtype, device=self.device)
-            ok = None if k is None else torch.empty(ks, dtype=dtype, device=self.device)
-        else:
-            oq, ok = out
-            if (ok is None) != (k is None):
-                raise ValueError("out must have a tensor for k where there is one")
-        native.dion_qknorm_forward(self.handle, shape, hq, hk, self._weight("wq", wq), self._weight("wk", wk),
-                                   self._heads("out[0]", oq, qs, dtype), self._heads("out[1]", ok, ks, dtype), s)
+        oq, hoq, ok, hok = self._outputs(out, qs, ks, dtype)
+        native.dion_qknorm_forward(self.handle, shape, hq, hk, self._weight("wq", wq), self._weight("wk", wk), hoq, hok, s)
         return oq, ok
 
     def backward(self, gq, gk, q, k=None, wq=None, wk=None, positions=None, out=None, stream: Optional[int] = None):
@@ -230,18 +237,15 @@ class QKNormPlan:
             raise ValueError("gk and k go together")
         hgq, hgk = self._heads("gq", gq, qs, dtype), self._heads("gk", gk, ks, dtype)
         s = _stream(self._index, stream, out is not None)
+        dq, hdq, dk, hdk = self._outputs(None if out is None else out[:2], qs, ks, dtype)
+        pwq, pwk = self._weight("wq", wq), self._weight("wk", wk)
         if out is None:
-            dq = torch.empty(qs, dtype=dtype, device=self.device)
-            dk = None if k is None else torch.empty(ks, dtype=dtype, device=self.device)
             dwq = None if wq is None else torch.empty_like(wq)
             dwk = None if wk is None else torch.empty_like(wk)
         else:
-            dq, dk, dwq, dwk = out
-            if (dk is None) != (k is None):
-                raise ValueError("out must have a tensor for k where there is one")
-        native.dion_qknorm_backward(self.handle, shape, hgq, hgk, hq, hk, self._weight("wq", wq), self._weight("wk", wk),
-                                    self._heads("out[0]", dq, qs, dtype), self._heads("out[1]", dk, ks, dtype),
-                                    self._weight("out[2]", dwq), self._weight("out[3]", dwk), s)
+            dwq, dwk = out[2:]
+        native.dion_qknorm_backward(self.handle, shape, hgq, hgk, hq, hk, pwq, pwk, hdq, hdk, self._weight("out[2]", dwq),
+                                    self._weight("out[3]", dwk), s)
         return dq, dk, dwq, dwk
 
     def close(self) -> None:
