@@ -1,0 +1,129 @@
+"""Trains a small GPT from a teacher's top logits with the library's operators and optimizer step.
+
+    python examples/distill_gpt.py [--steps 60]
+
+The student's embedding lookup, query/key norm with rotation and distillation loss are the library's
+operators; their gradients and torch's give each matrix its gradient, which dion_step applies (Dion
+for the matrices, torch's AdamW for the table and the norm weights).  The table is tied to the
+output layer: the lookup's gradient is added to the output's.  Teacher and text are synthetic: a frozen
+model of the same shape on tokens drawn with the 1/rank law.
+"""
+from __future__ import annotations
+
+import argparse
+import math
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+import paper_2512_13728_gb300 as cd  # noqa: E402
+
+DTYPE = torch.bfloat16
+
+
+class QKNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, plan, q, k, wq, wk):
+        ctx.plan = plan
+        ctx.save_for_backward(q, k, wq, wk)
+        return plan.forward(q, k, wq, wk)
+
+    @staticmethod
+    def backward(ctx, gq, gk):
+        return (None, *ctx.plan.backward(gq, gk, *ctx.saved_tensors))
+
+
+class Distill(torch.autograd.Function):
+    """Sum over the rows; the gradient comes with the loss."""
+
+    @staticmethod
+    def forward(ctx, logits, ids, teacher, temperature, weights):
+        loss, grad = cd.distill_loss_grad(logits, ids, teacher, temperature, weights=weights)
+        ctx.save_for_backward(grad)
+        return loss.sum()
+
+    @staticmethod
+    def backward(ctx, g):
+        return ctx.saved_tensors[0] * g.to(DTYPE), None, None, None, None
+
+
+class GPT:
+    """Six matrices per block (fp32 parameters with bf16 copies for the products), tied table, norm weights."""
+
+    def __init__(self, vocab=503, dim=128, heads=4, blocks=2, batch=8, tokens=64, seed=0, gain=1.0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        def draw(*shape, std):
+            return torch.randn(shape, generator=g, device="cuda") * std
+        self.heads, self.blocks, self.dim, self.vocab = heads, blocks, dim, vocab
+        shapes = [(dim, dim)] * 4 + [(dim, 4 * dim), (4 * dim, dim)]
+        self.X = [draw(m, n, std=gain / math.sqrt(m)) for _ in range(blocks) for m, n in shapes]
+        self.G = [torch.zeros(x.shape, dtype=DTYPE, device="cuda") for x in self.X]
+        self.W = [x.to(DTYPE).requires_grad_() for x in self.X]
+        for w, grad in zip(self.W, self.G):
+            w.grad = grad  # torch adds each step's gradient into the buffer that the optimizer plan reads
+        self.table = draw(vocab, dim, std=1 / math.sqrt(dim)).requires_grad_()
+        self.norms = [torch.ones(dim // heads, device="cuda").requires_grad_() for _ in range(2 * blocks)]
+        self.embed = cd.EmbedPlan(vocab, dim, batch * tokens)
+        self.qk = cd.QKNormPlan(dim // heads)
+        self.scale = math.sqrt(dim)
+
+    def logits(self, tokens):
+        """Logits [tokens, vocab], and the lookup's output, whose gradient the backward pass leaves."""
+        b, t = tokens.shape
+        x = x0 = self.embed.lookup(tokens, self.table.detach(), self.scale, dtype=DTYPE).requires_grad_()
+        for i in range(self.blocks):
+            wq, wk, wv, wo, w1, w2 = self.W[6 * i:6 * i + 6]
+            y = torch.nn.functional.rms_norm(x, (self.dim,))
+            q, k, v = (torch.matmul(y, w).view(b, t, self.heads, -1) for w in (wq, wk, wv))
+            q, k = QKNorm.apply(self.qk, q, k, self.norms[2 * i], self.norms[2 * i + 1])
+            a = torch.nn.functional.scaled_dot_product_attention(*(z.transpose(1, 2) for z in (q, k, v)), is_causal=True)
+            x = x + a.transpose(1, 2).reshape(b, t, self.dim) @ wo
+            x = x + torch.nn.functional.gelu(torch.nn.functional.rms_norm(x, (self.dim,)) @ w1) @ w2
+        y = torch.nn.functional.rms_norm(x, (self.dim,)).view(b * t, self.dim)
+        return y @ self.table.to(DTYPE).t(), x0
+
+
+def train(steps=60, batch=8, tokens=64, top=16, temperature=2.0, rank=32, lr=0.02, log=print):
+    """Losses per token, one for each step."""
+    teacher, student = GPT(seed=1, gain=1.5, batch=batch, tokens=tokens), GPT(seed=2, batch=batch, tokens=tokens)
+    X, vocab = student.X, student.vocab
+    Q = [torch.linalg.qr(torch.randn(x.shape[1], rank, device="cuda"))[0].contiguous() for x in X]
+    plan = cd.Plan(X, [torch.zeros_like(x) for x in X], Q, student.G, [0.5] * len(X), cd.DION_PREC_BF16)
+    scalars = torch.optim.AdamW([student.table, *student.norms], lr=3e-3, weight_decay=0.0)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    losses = []
+    for step in range(1, steps + 1):
+        text = torch.exp(torch.rand(batch, tokens, generator=g, device="cuda") * math.log(vocab)).long() - 1
+        with torch.no_grad():
+            best = teacher.logits(text)[0].topk(top, 1)
+        weights = torch.full((batch * tokens,), 1 / (batch * tokens), device="cuda")
+        logits, x0 = student.logits(text)
+        loss = Distill.apply(logits, best.indices, best.values, temperature, weights)
+        loss.backward()
+        # the tied table: the lookup's gradient goes on top of the output layer's
+        student.embed.gradient(text, x0.grad, student.scale, out=student.table.grad, accumulate=True)
+        eta = cd.lr_schedule(step, steps, lr, 0.1, 0.2)
+        plan.step(cd.hparams(eta=eta, step=step))
+        scalars.step()
+        scalars.zero_grad()
+        with torch.no_grad():
+            for w, x, grad in zip(student.W, X, student.G):
+                w.copy_(x)
+                grad.zero_()
+        losses.append(loss.detach())
+        if log and (step % 10 == 0 or step == 1):
+            log(f"step {step:4d}  loss {float(losses[-1]):.4f}")
+    torch.cuda.synchronize()
+    if plan.device_status() != 0:
+        raise RuntimeError("the optimizer step reported a device error")
+    plan.close()
+    return [float(v) for v in losses]
+
+
+if __name__ == "__main__":
+    ap = argparse.ArgumentParser()
+    ap.add_argument("--steps", type=int, default=60)
+    train(ap.parse_args().steps)
