@@ -60,13 +60,6 @@ def _ld(name: str, t, index: int, cols: int) -> int:
     return st[0] if st[0] > cols else cols  # torch leaves any stride on a single row
 
 
-def _indices(name: str, t, index: int) -> int:
-    code = _INDEX.get(t.dtype)
-    if code is None or t.get_device() != index:
-        raise ValueError(f"{name} must be an int32 or int64 tensor on cuda:{index}")
-    return code
-
-
 def _plan_device(device) -> "torch.device":
     if device is None:
         return torch.device("cuda", torch.cuda.current_device())
@@ -86,16 +79,23 @@ class EmbedPlan:
         with torch.cuda.device(self.device):
             self.handle = native.dion_embed_plan_create(vocab, dim, max_tokens)
 
+    def _tokens(self, tokens, stream):
+        """Index type, count and address of the tokens (contiguous; torch copies where they are not)."""
+        kind = _INDEX.get(tokens.dtype)
+        if kind is None or tokens.get_device() != self._index:
+            raise ValueError(f"tokens must be an int32 or int64 tensor on {self.device}")
+        n = tokens.numel()
+        flat = tokens if tokens.is_contiguous() else _flat("tokens", tokens, (n,), stream)
+        return kind, n, flat
+
     def lookup(self, tokens, table, scale: float = 1.0, out=None, dtype=None, stream: Optional[int] = None):
         """scale * table[tokens], shape tokens.shape + (dim,), of `dtype` (the table's by default)."""
         index, dim = self._index, self.dim
-        kind = _indices("tokens", tokens, index)
+        kind, n, flat = self._tokens(tokens, stream)
         ldt = _ld("table", table, index, dim)
         if table.shape[0] != self.vocab:
             raise ValueError(f"table must be {self.vocab} x {dim}")
         s = _stream(index, stream, out is not None)
-        n = tokens.numel()
-        flat = _flat("tokens", tokens, (n,), stream)
         if out is None:
             out = torch.empty((*tokens.shape, dim), dtype=dtype or table.dtype, device=self.device)
             ldo = dim
@@ -112,12 +112,10 @@ class EmbedPlan:
         """Gradient of the table, vocab x dim, of `dtype` (float32 by default), from the gradient `grad`
         of the lookup's output.  accumulate: added to `out`, of which only the tokens' rows are touched."""
         index, dim = self._index, self.dim
-        kind = _indices("tokens", tokens, index)
+        kind, n, flat = self._tokens(tokens, stream)
         if grad.shape[:-1] != tokens.shape:
             raise ValueError("grad must have the shape of tokens, and dim")
         s = _stream(index, stream, out is not None)
-        n = tokens.numel()
-        flat = _flat("tokens", tokens, (n,), stream)
         rows = grad if grad.dim() == 2 else _flat("grad", grad, (n, grad.shape[-1]), stream)
         ldg = _ld("grad", rows, index, dim)
         if out is None:
@@ -158,7 +156,7 @@ class QKNormPlan:
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, theta: float = 10000.0, interleaved: bool = False,
                  eps: float = 1e-6, inv_freq=None, device=None):
         self.device = _plan_device(device)
-        self.head_dim = head_dim
+        self.head_dim, self._wshape = head_dim, (head_dim,)
         self._index = self.device.index
         rotary_dim = head_dim if rotary_dim is None else rotary_dim
         if inv_freq is not None and len(inv_freq) != rotary_dim // 2:
@@ -171,73 +169,74 @@ class QKNormPlan:
         if t is None:
             return None
         st = t.stride()
-        if t.shape != shape or t.dtype != dtype or t.get_device() != self._index or st[-1] != 1:
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index or st[-1] != 1:
             raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} on {self.device} with contiguous heads")
-        return _HEADS.pack(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
+        return _HEADS.pack(t.data_ptr(), *st[:3]) if len(st) == 4 else _HEADS.pack(t.data_ptr(), 0, *st[:2])
 
-    def _outputs(self, out, qs, ks, dtype):
-        """The outputs of q's and k's shapes (those given, or new ones), each with its packed dion_heads."""
-        if out is not None:
-            oq, ok = out
-            if (ok is None) != (ks is None):
-                raise ValueError("out must have a tensor for k where there is one")
-            return oq, self._heads("out[0]", oq, qs, dtype), ok, self._heads("out[1]", ok, ks, dtype)
-        d = self.head_dim
-        oq, ok, hok = torch.empty(qs, dtype=dtype, device=self.device), None, None
-        if ks is not None:
-            ok = torch.empty(ks, dtype=dtype, device=self.device)
-            hok = _HEADS.pack(ok.data_ptr(), ks[-3] * ks[-2] * d, ks[-2] * d, d)
-        return oq, _HEADS.pack(oq.data_ptr(), qs[-3] * qs[-2] * d, qs[-2] * d, d), ok, hok
-
-    def _shape(self, q, k, positions):
-        """A packed dion_qk_shape, and the dtype."""
-        dims, dtype = q.shape, q.dtype
-        if len(dims) not in (3, 4) or dims[-1] != self.head_dim or dtype not in _DTYPES:
-            raise ValueError(f"q must be a float32 or bfloat16 tensor [batch, tokens, heads, {self.head_dim}]")
-        batch, tokens = dims[0] if len(dims) == 4 else 1, dims[-3]
-        kv_heads = 0
+    def _inputs(self, q, k, positions):
+        """A packed dion_qk_shape, and q's and k's packed dion_heads."""
+        dims, st, dtype, index = q.shape, q.stride(), q.dtype, self._index
+        code, n = _DTYPES.get(dtype), len(dims)
+        if n not in (3, 4) or code is None or dims[-1] != self.head_dim or st[-1] != 1 or q.get_device() != index:
+            raise ValueError(f"q must be a float32 or bfloat16 tensor [batch, tokens, heads, {self.head_dim}] on {self.device} "
+                             "with contiguous heads")
+        if n == 4:
+            batch, tokens, heads, _ = dims
+            hq = _HEADS.pack(q.data_ptr(), *st[:3])
+        else:
+            batch, (tokens, heads, _) = 1, dims
+            hq = _HEADS.pack(q.data_ptr(), 0, *st[:2])
+        kv_heads, hk = 0, None
         if k is not None:
             kd = k.shape
-            if len(kd) != len(dims) or kd[:-2] != dims[:-2] or kd[-1] != dims[-1]:
-                raise ValueError("q and k must agree in batch, tokens and head_dim")
+            if len(kd) != n or kd[0] != dims[0] or (n == 4 and kd[1] != tokens):
+                raise ValueError("q and k must agree in batch and tokens")
             kv_heads = kd[-2]
-        ptr = kind = stride = 0
-        if positions is not None:
-            kind = _indices("positions", positions, self._index)
-            ps, pd = positions.stride(), positions.shape
-            if (pd != dims[:-2] and pd != (tokens,)) or (tokens > 1 and ps[-1] != 1):
-                raise ValueError("positions must be [batch, tokens] or [tokens], contiguous over tokens")
-            ptr, stride = positions.data_ptr(), ps[0] if len(ps) == 2 else 0
-        return _QK_SHAPE.pack(batch, tokens, dims[-2], kv_heads, _DTYPES[dtype], kind, ptr, stride), dtype
+            hk = self._heads("k", k, (*dims[:-2], kv_heads, self.head_dim), dtype)
+        if positions is None:
+            return _QK_SHAPE.pack(batch, tokens, heads, kv_heads, code, 0, 0, 0), hq, hk
+        kind, ps, pd = _INDEX.get(positions.dtype), positions.stride(), positions.shape
+        rows = len(pd) == 2
+        if kind is None or positions.get_device() != index or pd != ((batch, tokens) if rows else (tokens,)) or \
+                (n == 3 and rows) or (tokens > 1 and ps[-1] != 1):
+            raise ValueError("positions must be an int32 or int64 tensor [batch, tokens] or [tokens] on q's device, contiguous "
+                             "over tokens")
+        return _QK_SHAPE.pack(batch, tokens, heads, kv_heads, code, kind, positions.data_ptr(), ps[0] if rows else 0), hq, hk
+
+    def _outputs(self, out, q, k):
+        """The outputs of q's and k's shapes (those given, or new ones), each with its packed dion_heads."""
+        if out is None:
+            out = torch.empty_like(q), None if k is None else torch.empty_like(k)
+        oq, ok = out
+        if (ok is None) != (k is None):
+            raise ValueError("out must have a tensor for k where there is one")
+        return oq, self._heads("out[0]", oq, q.shape, q.dtype), ok, ok if k is None else self._heads("out[1]", ok, k.shape, k.dtype)
 
     def _weight(self, name: str, w):
         if w is None:
             return None
-        if w.dtype != torch.float32 or w.get_device() != self._index or w.shape != (self.head_dim,) or w.stride(0) != 1:
+        if w.dtype is not torch.float32 or w.get_device() != self._index or w.shape != self._wshape or not w.is_contiguous():
             raise ValueError(f"{name} must be a contiguous float32 tensor of {self.head_dim} elements on {self.device}")
         return w.data_ptr()
 
     def forward(self, q, k=None, wq=None, wk=None, positions=None, out=None, stream: Optional[int] = None):
-        """(q', k'), written into `out` (a pair; q and k themselves: in place) or new contiguous tensors."""
-        shape, dtype = self._shape(q, k, positions)
-        qs, ks = q.shape, None if k is None else k.shape
-        hq, hk = self._heads("q", q, qs, dtype), self._heads("k", k, ks, dtype)
+        """(q', k'), written into `out` (a pair; q and k themselves: in place) or into new tensors as
+        torch.empty_like lays them out."""
+        shape, hq, hk = self._inputs(q, k, positions)
         s = _stream(self._index, stream, out is not None)
-        oq, hoq, ok, hok = self._outputs(out, qs, ks, dtype)
+        oq, hoq, ok, hok = self._outputs(out, q, k)
         native.dion_qknorm_forward(self.handle, shape, hq, hk, self._weight("wq", wq), self._weight("wk", wk), hoq, hok, s)
         return oq, ok
 
     def backward(self, gq, gk, q, k=None, wq=None, wk=None, positions=None, out=None, stream: Optional[int] = None):
         """(dq, dk, dwq, dwk) from the gradients of forward's outputs and forward's inputs; the last two are
         None where the weight is.  `out`: the four to write into (dq, dk may be gq, gk: in place)."""
-        shape, dtype = self._shape(q, k, positions)
-        qs, ks = q.shape, None if k is None else k.shape
-        hq, hk = self._heads("q", q, qs, dtype), self._heads("k", k, ks, dtype)
+        shape, hq, hk = self._inputs(q, k, positions)
         if (gk is None) != (k is None):
             raise ValueError("gk and k go together")
-        hgq, hgk = self._heads("gq", gq, qs, dtype), self._heads("gk", gk, ks, dtype)
+        hgq, hgk = self._heads("gq", gq, q.shape, q.dtype), gk if k is None else self._heads("gk", gk, k.shape, k.dtype)
         s = _stream(self._index, stream, out is not None)
-        dq, hdq, dk, hdk = self._outputs(None if out is None else out[:2], qs, ks, dtype)
+        dq, hdq, dk, hdk = self._outputs(None if out is None else out[:2], q, k)
         pwq, pwk = self._weight("wq", wq), self._weight("wk", wk)
         if out is None:
             dwq = None if wq is None else torch.empty_like(wq)
@@ -262,28 +261,28 @@ class QKNormPlan:
 
 def _distill(logits, ids, teacher, temperature, labels, hard, weights):
     """A packed dion_distill, the device index and the rows."""
-    index = logits.get_device()
-    if index < 0 or logits.dim() != 2:
+    index, shape = logits.get_device(), logits.shape
+    if index < 0 or len(shape) != 2:
         raise ValueError("logits must be a 2-D tensor on a GPU")
-    rows, vocab = logits.shape
+    rows, vocab = shape
     ld = _ld("logits", logits, index, vocab)
     top = ids_ptr = ld_ids = id_kind = teacher_ptr = ld_teacher = teacher_code = 0
     if ids is not None and teacher is not None:
-        if ids.shape != teacher.shape or ids.dim() != 2 or ids.shape[0] != rows:
+        ts, st, id_kind = ids.shape, ids.stride(), _INDEX.get(ids.dtype)
+        if len(ts) != 2 or ts[0] != rows or teacher.shape != ts:
             raise ValueError("ids and teacher must both be [rows, top]")
-        id_kind, top = _indices("ids", ids, index), ids.shape[1]
-        st = ids.stride()
-        if top > 1 and st[1] != 1:
-            raise ValueError("ids must be row-major")
+        top = ts[1]
+        if id_kind is None or ids.get_device() != index or (top > 1 and st[1] != 1):
+            raise ValueError("ids must be a row-major int32 or int64 tensor on the logits' device")
         ld_teacher, teacher_code = _ld("teacher", teacher, index, top), _DTYPES[teacher.dtype]
         ids_ptr, ld_ids, teacher_ptr = ids.data_ptr(), st[0] if st[0] > top else top, teacher.data_ptr()
     elif ids is not None or teacher is not None or hard < 1:
         raise ValueError("ids and teacher go together, and are needed unless hard is 1")
     label_ptr = label_kind = weight_ptr = 0
     if labels is not None:
-        label_kind = _indices("labels", labels, index)
-        if labels.shape != (rows,) or (rows > 1 and labels.stride(0) != 1):
-            raise ValueError("labels must be a contiguous tensor [rows]")
+        label_kind = _INDEX.get(labels.dtype)
+        if label_kind is None or labels.get_device() != index or labels.shape != (rows,) or not labels.is_contiguous():
+            raise ValueError("labels must be a contiguous int32 or int64 tensor [rows] on the logits' device")
         label_ptr = labels.data_ptr()
     if weights is not None:
         weight_ptr = _row_values("weights", weights, rows, index)
@@ -292,7 +291,7 @@ def _distill(logits, ids, teacher, temperature, labels, hard, weights):
 
 
 def _row_values(name: str, t, rows: int, index: int) -> int:
-    if t.dtype != torch.float32 or t.get_device() != index or t.shape != (rows,) or (rows > 1 and t.stride(0) != 1):
+    if t.dtype is not torch.float32 or t.get_device() != index or t.shape != (rows,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor [rows]")
     return t.data_ptr()
 
@@ -326,7 +325,7 @@ def distill_loss_grad(logits, ids, teacher, temperature: float = 1.0, labels=Non
     s = _stream(index, stream, out is not None)
     if out is None:
         loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
-        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        grad = torch.empty_like(logits)
     else:
         loss, grad = out
         if grad.dtype != logits.dtype or grad.shape != logits.shape:
