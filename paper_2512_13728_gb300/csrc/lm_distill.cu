@@ -23,6 +23,8 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxWorkers = 12, kMaxTeachers = 3;  // warps of the gradient's blocks
+constexpr int kShortThreads = 256;
+constexpr int kShortChunks = 512;                   // of a row that a warp takes alone (8 KB)
 constexpr int kGradThreads = 512;                   // of a block; two blocks per SM
 constexpr int kLossThreads = 256;
 constexpr int kMaxCluster = 8;
@@ -417,6 +419,47 @@ __device__ __forceinline__ float base_gradient(const Factors &f, float z, float 
   return g;
 }
 
+// Whether a column of [lo, hi) comes twice among a row's entries: a bit for each, set and cleared by its
+// entries.  One warp.
+__device__ __forceinline__ bool comes_twice(const Entries &E, int entries, uint32_t *bitmap, int lo, int hi) {
+  bool twice = false;
+#pragma unroll 4
+  for (int k = threadIdx.x & 31; k < entries; k += 32) {
+    const int j = E.col[k];
+    const uint32_t bit = 1u << ((j - lo) & 31);
+    if (j >= 0 && j >= lo && j < hi) twice |= (atomicOr(&bitmap[(j - lo) >> 5], bit) & bit) != 0;
+  }
+  twice = __any_sync(0xffffffffu, twice);
+#pragma unroll 4
+  for (int k = threadIdx.x & 31; k < entries; k += 32) {
+    const int j = E.col[k];
+    if (j >= 0 && j >= lo && j < hi) bitmap[(j - lo) >> 5] = 0;
+  }
+  __syncwarp();
+  return twice;
+}
+
+// The entries' columns of [lo, hi) over what was written there.  One warp, behind a barrier with the
+// threads that wrote.
+template <class T, bool TWO>
+__device__ __forceinline__ void write_entries(const Args &A, const Entries &E, const Factors &f, float w, T *g, int lo, int hi,
+                                              bool twice, int entries) {
+  const int top = A.soft ? (int)A.d.top : 0;
+#pragma unroll 4
+  for (int k = threadIdx.x & 31; k < entries; k += 32) {
+    const int j = E.col[k];
+    float off = E.share(A, k, top);
+    bool write = j >= 0 && j >= lo && j < hi;
+    if (twice && write) {  // an entry that comes several times: the first writes, with all their shares
+      off = 0.f;
+      for (int i = 0; i < entries; ++i)
+        if (E.col[i] == j) write &= i >= k, off += E.share(A, i, top);
+    }
+    if (write) store_one(g + j, base_gradient<TWO>(f, E.zval[k], A.c) - w * off);
+  }
+  __syncwarp();  // the entries are read; the next row's take their place
+}
+
 // Bounded wait for the statistics of every block of the cluster.
 __device__ __forceinline__ bool wait_stats(uint64_t *bar, uint32_t parity) {
   const uint64_t t0 = tc::globaltimer_ns();
@@ -614,21 +657,8 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_kernel(const __grid_cons
       const int lo = r.column(r.lo), hi = r.column(r.hi);
       bool twice = false;
       if (w != 0.f) {
-        // whether a column of this block's part comes twice: a bit for each, set and cleared by its
-        // entries (between a row's barrier and the next one the bits are this teacher's alone)
-#pragma unroll 4
-        for (int k = lane; k < entries; k += 32) {
-          const int j = E.col[k];
-          const uint32_t bit = 1u << ((j - lo) & 31);
-          if (j >= 0 && j >= lo && j < hi) twice |= (atomicOr(&bitmap[(j - lo) >> 5], bit) & bit) != 0;
-        }
-        twice = __any_sync(0xffffffffu, twice);
-#pragma unroll 4
-        for (int k = lane; k < entries; k += 32) {
-          const int j = E.col[k];
-          if (j >= 0 && j >= lo && j < hi) bitmap[(j - lo) >> 5] = 0;
-        }
-        __syncwarp();
+        // (between a row's barrier and the next one the bits are this teacher's alone)
+        twice = comes_twice(E, entries, bitmap, lo, hi);
       }
       barrier(n + 1);
       if (rank == 0) {
@@ -636,25 +666,96 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_kernel(const __grid_cons
         if (lane == 0) A.loss[row] = loss;
       }
       if (w != 0.f) {
-        T *g = static_cast<T *>(A.grad) + row * A.ldg;
-        const Factors f = factors<TWO>(A, terms, s, w);
-#pragma unroll 4
-        for (int k = lane; k < entries; k += 32) {
-          const int j = E.col[k];
-          float off = E.share(A, k, top);
-          bool write = j >= 0 && j >= lo && j < hi;
-          if (twice && write) {  // an entry that comes several times: the first writes, with all their shares
-            off = 0.f;
-            for (int i = 0; i < entries; ++i)
-              if (E.col[i] == j) write &= i >= k, off += E.share(A, i, top);
-          }
-          if (write) store_one(g + j, base_gradient<TWO>(f, E.zval[k], A.c) - w * off);
-        }
-        __syncwarp();  // the entries are read; the next row takes their place
+        write_entries<T, TWO>(A, E, factors<TWO>(A, terms, s, w), w, static_cast<T *>(A.grad) + row * A.ldg, lo, hi, twice, entries);
       }
     }
   }
   if (A.cluster > 1) tc::cluster_sync();  // nothing is sent to a block that is gone
+}
+
+// ----------------------------------------------------------------------------- short rows ---
+// A warp per row, with or without gradient: the row in its shared memory (gradient) or straight from
+// global memory, no barriers.  For rows of up to kShortChunks chunks, of which a block would spend its time
+// waiting for the teacher's entries.
+template <class T, bool GRAD, bool TWO>
+__global__ void __launch_bounds__(kShortThreads, 4) short_kernel(const __grid_constant__ Args A) {
+  constexpr int N = 16 / sizeof(T);
+  extern __shared__ uint4 smem[];
+  const dion_distill &d = A.d;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, top = A.soft ? (int)d.top : 0, entries = top + (A.hard ? 1 : 0);
+  // of this warp: the row, a bit for each column (both only for the gradient), the entries
+  uint4 *mine = smem + warp * A.part;
+  uint32_t *bitmap = reinterpret_cast<uint32_t *>(smem + kShortThreads / 32 * (GRAD ? A.part : 0)) + warp * A.bitmap;
+  const Entries E(reinterpret_cast<float *>(bitmap + (kShortThreads / 32 - warp) * A.bitmap) + warp * 3 * (top + 1), top + 1);
+  if (GRAD)
+    for (int i = lane; i < A.bitmap; i += 32) bitmap[i] = 0;
+  chain_enter();
+  const int64_t row = (int64_t)blockIdx.x * (kShortThreads / 32) + warp;
+  if (row >= d.rows) return;
+  const float w = d.weights ? d.weights[row] : 1.f;
+  const Row<T> r(A, row, 0);
+  T *g = GRAD ? static_cast<T *>(A.grad) + row * A.ldg : nullptr;
+  if (w == 0.f) {
+    if (lane == 0) A.loss[row] = 0.f;
+    if (GRAD)
+      for (int j = lane; j < r.vocab; j += 32) store_one(g + j, 0.f);
+    return;
+  }
+  Batch b = fetch_entries(A, row, 0);
+  const int32_t label = fetch_label(A, row);
+  if (GRAD)
+    for (int c = r.first(lane, 32); c < r.hi; c += 32) {
+      if (r.whole(c))
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(mine + c)), "l"(r.at(c)) : "memory");
+      else
+        mine[c] = r.edge(c);
+    }
+  float z[kBatch];
+  gather_logits<T>(A, row, b, z);
+  const RowTerms terms = set_entries<T>(A, row, E, b, z, label, label_logit<T>(A, row, label));
+  Stats s{-INFINITY, 0.f, 0.f};
+  asm volatile("cp.async.wait_all;" ::: "memory");  // each lane reads only what it copied itself
+  auto chunk = [&](int c) { return GRAD ? mine[c] : r.whole(c) ? *r.at(c) : r.edge(c); };
+  int c = r.first(lane, 32);
+  for (; c + 96 < r.hi; c += 128) {
+    Chunk<T> v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u].raw = chunk(c + 32 * u);
+    take<T, 4, TWO>(v, s, A.c);
+  }
+  for (; c < r.hi; c += 32) {
+    Chunk<T> v[1];
+    v[0].raw = chunk(c);
+    take<T, 1, TWO>(v, s, A.c);
+  }
+  s = merge_lanes<TWO>(s, A.c);
+  const float loss = w * row_loss<TWO>(A, E, terms, s);
+  if (lane == 0) A.loss[row] = loss;
+  if (!GRAD) return;
+  const Factors f = factors<TWO>(A, terms, s, w);
+  const bool zeros = !terms.soft && !terms.hard;
+  const bool same_place = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T)) == r.lead % N;
+  for (c = r.first(lane, 32); c < r.hi; c += 32) {
+    Chunk<T> x;
+    x.raw = mine[c];
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      unpack2(x.pair(i), v[2 * i], v[2 * i + 1]);
+#pragma unroll
+      for (int e = 2 * i; e < 2 * i + 2; ++e) v[e] = zeros ? 0.f : base_gradient<TWO>(f, v[e], A.c);
+    }
+    if (same_place && r.whole(c)) {
+      store_vec<T, N>(g + r.column(c), v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int j = r.column(c) + e;
+        if (j >= 0 && j < r.vocab) store_one(g + j, v[e]);
+      }
+    }
+  }
+  write_entries<T, TWO>(A, E, f, w, g, 0, r.vocab, comes_twice(E, entries, bitmap, 0, r.vocab), entries);
 }
 
 // ----------------------------------------------------------------------------- dispatch ---
@@ -707,11 +808,28 @@ int64_t row_chunks(const dion_distill *d) { return (d->vocab * element_bytes(d->
 int32_t part_of(int64_t chunks, int cluster) { return (int32_t)(((chunks + cluster - 1) / cluster + 7) / 8 * 8); }
 size_t entry_bytes(const Args &A) { return 12 * ((A.soft ? (size_t)A.d.top : 0) + 1); }
 
+template <bool GRAD>
+dion_status enqueue_short(Args A, int64_t chunks, cudaStream_t s) {
+  A.cluster = 1, A.part = part_of(chunks, 1);
+  A.bitmap = GRAD ? (int32_t)((A.d.vocab + 31) / 32) : 0;
+  const int64_t warps = kShortThreads / 32;
+  const size_t smem = warps * ((GRAD ? (size_t)A.part * 16 : 0) + 4 * (size_t)A.bitmap + entry_bytes(A));
+  const int64_t grid = (A.d.rows + warps - 1) / warps;
+  const bool two = two_softmaxes(A);
+  using BF = __nv_bfloat16;
+  const cudaError_t e =
+      A.d.dtype == DION_DTYPE_FP32
+          ? run(two ? short_kernel<float, GRAD, true> : short_kernel<float, GRAD, false>, A, grid, kShortThreads, smem, s)
+          : run(two ? short_kernel<BF, GRAD, true> : short_kernel<BF, GRAD, false>, A, grid, kShortThreads, smem, s);
+  return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
+}
+
 dion_status enqueue_loss(const dion_distill *d, float *loss, cudaStream_t s) {
   const int sms = num_sms();
   if (sms == 0) return DION_ERR_CUDA;
   Args A = make_args(d, loss);
   const int64_t chunks = row_chunks(d);
+  if (chunks <= kShortChunks && d->rows > 2 * sms) return enqueue_short<false>(A, chunks, s);
   A.cluster = 1;  // more blocks per row while the rows leave SMs idle and a thread has more than one round of chunks
   while (A.cluster < kMaxCluster && d->rows * A.cluster * 2 <= sms && chunks / A.cluster > 4 * kLossThreads) A.cluster *= 2;
   A.part = part_of(chunks, A.cluster);
@@ -732,6 +850,7 @@ dion_status enqueue_grad(const dion_distill *d, float *loss, void *grad, int64_t
   Args A = make_args(d, loss);
   A.grad = grad, A.ldg = ldg;
   const int64_t chunks = row_chunks(d);
+  if (chunks <= kShortChunks && d->rows > 2 * sms) return enqueue_short<true>(A, chunks, s);
   const int per_chunk = 16 / element_bytes(d->dtype);
   auto shape = [&](int cluster, int teachers) {
     A.cluster = cluster, A.teachers = teachers;
@@ -747,7 +866,9 @@ dion_status enqueue_grad(const dion_distill *d, float *loss, void *grad, int64_t
   size_t smem = shape(cluster, kMaxTeachers);
   if (smem + taken > kSmemPerSm) smem = shape(cluster, 2);
   if (smem + taken > kSmemPerSm) return DION_ERR_UNSUPPORTED;
-  const int64_t by_smem = (int64_t)(kSmemPerSm / (smem + taken));
+  // four blocks per SM at most: more would have one worker each (8192 rows of 8000 bf16 logits: 57 us with four,
+  // 86 with as many as fit, 67 with three)
+  const int64_t by_smem = std::min<int64_t>(4, (int64_t)(kSmemPerSm / (smem + taken)));
   // about 32 warps per SM; with many blocks per SM no less than eight chunks per thread
   const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kMaxWorkers, 32 / by_smem - A.teachers));
   const int workers = (int)std::min<int64_t>(want, std::max<int64_t>(1, (A.part / (d->rows * cluster <= sms ? 1 : 8) + 31) / 32));
