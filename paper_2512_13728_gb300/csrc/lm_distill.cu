@@ -785,6 +785,25 @@ cudaError_t run(void (*kernel)(P...), const Args &A, int64_t grid, int threads, 
   return e != cudaSuccess ? e : launch(kernel, grid, threads, smem, s, A.cluster, A);
 }
 
+// Clusters of a kernel that run at the same time on an otherwise empty GPU.
+cudaError_t resident_clusters(void (*kernel)(Args), int cluster, int threads, size_t smem, int64_t *count) {
+  cudaError_t e = allow_smem(kernel, smem);
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = (unsigned)cluster;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)cluster);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+  *count = std::max(n, 1);
+  return e;
+}
+
 int num_sms() {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
@@ -874,12 +893,18 @@ dion_status enqueue_grad(const dion_distill *d, float *loss, void *grad, int64_t
   const int workers = (int)std::min<int64_t>(want, std::max<int64_t>(1, (A.part / (d->rows * cluster <= sms ? 1 : 8) + 31) / 32));
   const int threads = (workers + A.teachers) * 32;
   const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(by_smem, 1024 / threads));
-  const int64_t clusters = std::min<int64_t>(d->rows, std::max<int64_t>(1, sms * resident / cluster));
+  int64_t clusters = std::max<int64_t>(1, sms * resident / cluster);
   const bool two = two_softmaxes(A);
   using BF = __nv_bfloat16;
-  const cudaError_t e = d->dtype == DION_DTYPE_FP32
-                            ? run(two ? grad_kernel<float, true> : grad_kernel<float, false>, A, clusters * cluster, threads, smem, s)
-                            : run(two ? grad_kernel<BF, true> : grad_kernel<BF, false>, A, clusters * cluster, threads, smem, s);
+  void (*kernel)(Args) = d->dtype == DION_DTYPE_FP32 ? (two ? grad_kernel<float, true> : grad_kernel<float, false>)
+                                                     : (two ? grad_kernel<BF, true> : grad_kernel<BF, false>);
+  if (cluster > 1 && d->rows > clusters / 2) {
+    // clusters lie within a GPC, whose SMs they need not divide: one more than fit would run alone after the others
+    const cudaError_t e = resident_clusters(kernel, cluster, threads, smem, &clusters);
+    if (e != cudaSuccess) return DION_ERR_CUDA;
+  }
+  clusters = std::min<int64_t>(d->rows, clusters);
+  const cudaError_t e = run(kernel, A, clusters * cluster, threads, smem, s);
   return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
 }
 
