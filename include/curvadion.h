@@ -330,8 +330,8 @@ enum { DION_INDEX_INT32 = 0, DION_INDEX_INT64 = 1 };
  * with leading dimensions ld >= dim, types DION_DTYPE_* each on its own.  Outputs must not overlap
  * inputs.
  * Errors: INVALID_ARG (NULL pointer, size < 0 or ld < dim, unknown type, scale not finite,
- * num_tokens > max_tokens in the gradient), UNSUPPORTED (vocab, max_tokens or dim of 2^30 or more),
- * ALIGNMENT (pointer not a multiple of its element), CUDA. */
+ * num_tokens > max_tokens in the gradient), UNSUPPORTED (vocab, max_tokens or tokens of 2^30 or more, dim
+ * of 2^28 or more), ALIGNMENT (pointer not a multiple of its element), CUDA. */
 typedef struct dion_embed_plan dion_embed_plan;
 dion_status dion_embed_plan_create(int64_t vocab, int64_t dim, int64_t max_tokens, dion_embed_plan **out);
 dion_status dion_embed_lookup(dion_embed_plan *plan, const void *tokens, int32_t token_dtype, int64_t num_tokens,
@@ -359,7 +359,7 @@ void dion_embed_plan_destroy(dion_embed_plan *plan);
  * positions: index (b, t) at positions[b * position_batch_stride + t]; NULL: the position of token t is t.
  * An output may be its own input (the same dion_heads: in place); otherwise they must not overlap.
  * Errors: INVALID_ARG (NULL pointer, size out of range, unknown type, eps < 0 or not finite, theta <= 0),
- * UNSUPPORTED (head_dim > 256, more than 2048 heads of a kind, or more than 2^40 elements), ALIGNMENT (pointer not a multiple of its
+ * UNSUPPORTED (head_dim > 256, more than 2048 heads of a kind, 2^31 tokens or more), ALIGNMENT (pointer not a multiple of its
  * element), CUDA. */
 typedef struct dion_qknorm_plan dion_qknorm_plan;
 typedef struct {

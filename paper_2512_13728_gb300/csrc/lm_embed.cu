@@ -558,7 +558,7 @@ cudaError_t with_types(int32_t a, int32_t b, F &&f) {
   return b == DION_DTYPE_FP32 ? f(BF(), float()) : f(BF(), BF());
 }
 
-constexpr int64_t kSizeLimit = (int64_t)1 << 30;
+constexpr int64_t kSizeLimit = (int64_t)1 << 30, kDimLimit = (int64_t)1 << 28;
 
 dion_status check_rows(int64_t n, int64_t dim, const void *p, int32_t dtype, int64_t ld) {
   if (!is_dtype(dtype) || (n > 0 && !p) || ld < dim) return DION_ERR_INVALID_ARG;
@@ -581,7 +581,7 @@ dion_status dion_embed_plan_create(int64_t vocab, int64_t dim, int64_t max_token
   if (!out) return DION_ERR_INVALID_ARG;
   *out = nullptr;
   if (vocab < 1 || dim < 1 || max_tokens < 0) return DION_ERR_INVALID_ARG;
-  if (vocab >= kSizeLimit || dim >= kSizeLimit || max_tokens >= kSizeLimit) return DION_ERR_UNSUPPORTED;
+  if (vocab >= kSizeLimit || dim >= kDimLimit || max_tokens >= kSizeLimit) return DION_ERR_UNSUPPORTED;
   dion_embed_plan *p = new (std::nothrow) dion_embed_plan();
   if (!p) return DION_ERR_CUDA;
   p->vocab = vocab, p->dim = dim, p->max_tokens = max_tokens;

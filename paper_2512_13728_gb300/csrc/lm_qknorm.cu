@@ -83,9 +83,11 @@ __device__ __forceinline__ void pair_place(int u, int dim, int half, int &at, in
 // A lane's pairs of a head are NC chunks of V, `group` lanes apart; V divides half and dim / 2 - half unless
 // interleaved, when a chunk's pairs are 2 V neighbouring elements.  In memory and in the ring a chunk is
 // two pieces of V elements (the pairs' firsts and seconds, or its two halves).
-template <class T, int V, int NC, bool INTER>
+template <class T_, int V, int NC, bool INTER_>
 struct Lane {
-  static constexpr int kPairs = NC * V, kPacks = kPairs / 2;
+  using T = T_;
+  static constexpr bool INTER = INTER_;
+  static constexpr int kWidth = V, kPairs = NC * V, kPacks = kPairs / 2;
   static constexpr int kPiece = V * (int)sizeof(T);   // bytes
   static constexpr int kStep = 2 * NC * 32 * kPiece;  // of a warp's ring, a step of one tensor
   int at[NC], apart[NC];  // the pieces' first elements in a head: at, at + apart
@@ -104,7 +106,7 @@ struct Lane {
     return ((threadIdx.x & (A.group - 1)) + n * A.group) * V;
   }
   // starts the copies of a head into a step of the ring; zeros where there is no head or chunk
-  __device__ __forceinline__ void copy(const T *x, bool on, char *step) const {
+  __device__ __forceinline__ void copy(const Args &A, const T *x, bool on, char *step) const {
     char *to = step + (threadIdx.x & 31) * kPiece;
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
@@ -124,7 +126,7 @@ struct Lane {
     }
   }
   // a step's pairs, packed in twos: firsts and seconds
-  __device__ __forceinline__ void read(const char *step, uint64_t (&a)[kPacks], uint64_t (&b)[kPacks]) const {
+  __device__ __forceinline__ void read(const Args &A, const char *step, uint64_t (&a)[kPacks], uint64_t (&b)[kPacks]) const {
     const char *from = step + (threadIdx.x & 31) * kPiece;
     float x[2][kPairs];
 #pragma unroll
@@ -144,7 +146,9 @@ struct Lane {
 #pragma unroll
     for (int i = 0; i < kPacks; ++i) a[i] = pack2(x[0][2 * i], x[0][2 * i + 1]), b[i] = pack2(x[1][2 * i], x[1][2 * i + 1]);
   }
-  __device__ __forceinline__ void store(T *y, const uint64_t (&a)[kPacks], const uint64_t (&b)[kPacks]) const {
+  __device__ __forceinline__ void store(const Args &A, T *y, bool on, const uint64_t (&a)[kPacks], const uint64_t (&b)[kPacks],
+                                        char *step) const {
+    if (!on) return;
     float x[2][kPairs];
 #pragma unroll
     for (int i = 0; i < kPacks; ++i) unpack2(a[i], x[0][2 * i], x[0][2 * i + 1]), unpack2(b[i], x[1][2 * i], x[1][2 * i + 1]);
@@ -176,6 +180,67 @@ struct Lane {
     }
 #pragma unroll
     for (int i = 0; i < kPacks; ++i) v[i] = pack2(x[2 * i], x[2 * i + 1]);
+  }
+};
+
+// Pairs whose firsts or seconds are aligned to two elements at most (a rotated part of 2 x 19 elements),
+// in heads that are whole 16-byte pieces: heads are copied and written in pieces, through the ring's
+// step, from which a lane picks its pairs one by one.  (16384 tokens of 8 + 4 heads of 256 in bf16, 102
+// rotated: 73 us; with accesses of one element to global memory 98 us.)
+template <class T_>
+struct StagedLane : Lane<T_, 1, 4, false> {
+  using Base = Lane<T_, 1, 4, false>;
+  using T = T_;
+  using Base::at, Base::apart, Base::has, Base::kPacks, Base::kPairs;
+  __device__ __forceinline__ StagedLane(const Args &A) : Base(A) {}
+  static __device__ __forceinline__ int head_bytes(const Args &A) { return A.dim * (int)sizeof(T); }
+  static __device__ __forceinline__ T *head_of(const Args &A, char *step) {
+    return reinterpret_cast<T *>(step + (threadIdx.x & 31) / A.group * head_bytes(A));
+  }
+  __device__ __forceinline__ void copy(const Args &A, const T *x, bool on, char *step) const {
+    char *head = reinterpret_cast<char *>(head_of(A, step));
+    for (int p = 16 * (threadIdx.x & (A.group - 1)); p < head_bytes(A); p += 16 * A.group)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(head + p)),
+                   "l"(reinterpret_cast<const char *>(x) + p), "r"(on ? 16 : 0)
+                   : "memory");
+  }
+  __device__ __forceinline__ void read(const Args &A, char *step, uint64_t (&a)[kPacks], uint64_t (&b)[kPacks]) const {
+    __syncwarp();  // each lane has waited for its own copies
+    const T *head = head_of(A, step);
+    float x[2][kPairs];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        Raw<T, 1> raw;
+        raw.w[0] = 0;
+        if (has[i]) raw.load(head + at[i] + h * apart[i]);
+        x[h][i] = raw.at(0);
+      }
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) a[i] = pack2(x[0][2 * i], x[0][2 * i + 1]), b[i] = pack2(x[1][2 * i], x[1][2 * i + 1]);
+  }
+  __device__ __forceinline__ void store(const Args &A, T *y, bool on, const uint64_t (&a)[kPacks], const uint64_t (&b)[kPacks],
+                                        char *step) const {
+    __syncwarp();  // the step is read
+    T *head = head_of(A, step);
+    if (on) {
+      float x[2][kPairs];
+#pragma unroll
+      for (int i = 0; i < kPacks; ++i) unpack2(a[i], x[0][2 * i], x[0][2 * i + 1]), unpack2(b[i], x[1][2 * i], x[1][2 * i + 1]);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float v[1] = {x[h][i]};
+          if (has[i]) store_vec<T, 1>(head + at[i] + h * apart[i], v);
+        }
+    }
+    __syncwarp();
+    if (on)
+      for (int p = 16 * (threadIdx.x & (A.group - 1)); p < head_bytes(A); p += 16 * A.group)
+        *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(y) + p) =
+            *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(head) + p);
   }
 };
 
@@ -284,9 +349,9 @@ __device__ __forceinline__ void wait_copies() {
 }
 
 // ------------------------------------------------------------------------------ forward ---
-template <class T, int V, int NC, bool INTER>
-__global__ void __launch_bounds__(kThreads, forward_blocks(NC * V)) forward_kernel(const __grid_constant__ Args A) {
-  using L = Lane<T, V, NC, INTER>;
+template <class L>
+__global__ void __launch_bounds__(kThreads, forward_blocks(L::kPairs)) forward_kernel(const __grid_constant__ Args A) {
+  using T = typename L::T;
   constexpr int S = kRing, P = L::kPacks;
   __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs];
   __shared__ __align__(16) char ring[kWarps][S][L::kStep];
@@ -304,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, forward_blocks(NC * V)) forward_kern
   int filled = 0, used = 0;  // places of the ring
   auto fill = [&] {
     if (ahead.on(A)) {
-      mine.copy(from, h0 + ahead.step * groups < U.heads, ring[warp][filled]);
+      mine.copy(A, from, h0 + ahead.step * groups < U.heads, ring[warp][filled]);
       positions[warp].copy(A, ahead);
       if (ahead.next(A, U))
         from = ahead.head<const T>(X, h0);
@@ -316,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, forward_blocks(NC * V)) forward_kern
   };
 #pragma unroll
   for (int k = 0; k < S - 1; ++k) fill();
-  stage_weights<INTER>(A, w);  // while the first steps are on their way
+  stage_weights<L::INTER>(A, w);  // while the first steps are on their way
   const float inv_dim = 1.f / (float)A.dim;
   uint64_t ac[P], bs[P], bc[P], as[P];  // of a token: wa cos, -wb sin, wb cos, wa sin
   while (at.on(A)) {
@@ -336,23 +401,21 @@ __global__ void __launch_bounds__(kThreads, forward_blocks(NC * V)) forward_kern
       }
     }
     uint64_t a[P], b[P], sum2 = 0, sum2b = 0;
-    mine.read(ring[warp][used], a, b);
-    used = used + 1 == S ? 0 : used + 1;
+    mine.read(A, ring[warp][used], a, b);
 #pragma unroll
     for (int i = 0; i < P; ++i) sum2 = fma2(a[i], a[i], sum2), sum2b = fma2(b[i], b[i], sum2b);
     float sum, more;
     unpack2(add2(sum2, sum2b), sum, more);
     const float r = rsqrtf(group_sum(sum + more, A.group) * inv_dim + A.eps);
     const uint64_t r2 = pack2(r, r);
-    if (h0 + at.step * groups < U.heads) {
-      uint64_t ya[P], yb[P];
+    uint64_t ya[P], yb[P];
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        ya[i] = mul2(r2, fma2(b[i], bs[i], mul2(a[i], ac[i])));
-        yb[i] = mul2(r2, fma2(a[i], as[i], mul2(b[i], bc[i])));
-      }
-      mine.store(to, ya, yb);
+    for (int i = 0; i < P; ++i) {
+      ya[i] = mul2(r2, fma2(b[i], bs[i], mul2(a[i], ac[i])));
+      yb[i] = mul2(r2, fma2(a[i], as[i], mul2(b[i], bc[i])));
     }
+    mine.store(A, to, h0 + at.step * groups < U.heads, ya, yb, ring[warp][used]);
+    used = used + 1 == S ? 0 : used + 1;
     if (at.next(A, U))
       to = at.head<T>(Y, h0);
     else
@@ -362,9 +425,9 @@ __global__ void __launch_bounds__(kThreads, forward_blocks(NC * V)) forward_kern
 }
 
 // ----------------------------------------------------------------------------- backward ---
-template <class T, int V, int NC, bool INTER>
-__global__ void __launch_bounds__(kThreads, backward_blocks(NC * V)) backward_kernel(const __grid_constant__ Args A) {
-  using L = Lane<T, V, NC, INTER>;
+template <class L>
+__global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward_kernel(const __grid_constant__ Args A) {
+  using T = typename L::T;
   constexpr int S = kRing, P = L::kPacks;
   __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs];
   __shared__ __align__(16) char ring[kWarps][S][2][L::kStep];
@@ -383,8 +446,8 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(NC * V)) backward_ke
   auto fill = [&] {
     if (ahead.on(A)) {
       const bool on = h0 + ahead.step * groups < U.heads;
-      mine.copy(from, on, ring[warp][filled][0]);
-      mine.copy(from_g, on, ring[warp][filled][1]);
+      mine.copy(A, from, on, ring[warp][filled][0]);
+      mine.copy(A, from_g, on, ring[warp][filled][1]);
       positions[warp].copy(A, ahead);
       if (ahead.next(A, U))
         from = ahead.head<const T>(X, h0), from_g = ahead.head<const T>(G, h0);
@@ -396,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(NC * V)) backward_ke
   };
 #pragma unroll
   for (int k = 0; k < S - 1; ++k) fill();
-  stage_weights<INTER>(A, w);  // while the first steps are on their way
+  stage_weights<L::INTER>(A, w);  // while the first steps are on their way
   const float inv_dim = 1.f / (float)A.dim;
   uint64_t c[P], s[P], ns[P], wa[P], wb[P], da[P], db[P];  // ns = -s; da, db: this lane's sums of dw
   mine.read_pairs(w[U.kind][0], A, wa);
@@ -414,9 +477,8 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(NC * V)) backward_ke
       for (int i = 0; i < P; ++i) ns[i] = mul2(s[i], pack2(-1.f, -1.f));
     }
     uint64_t a[P], b[P], ga[P], gb[P], sum2 = 0, sum2b = 0, dot2 = 0, dot2b = 0;
-    mine.read(ring[warp][used][0], a, b);
-    mine.read(ring[warp][used][1], ga, gb);
-    used = used + 1 == S ? 0 : used + 1;
+    mine.read(A, ring[warp][used][0], a, b);
+    mine.read(A, ring[warp][used][1], ga, gb);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const uint64_t oa = ga[i], ob = gb[i];
@@ -437,7 +499,8 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(NC * V)) backward_ke
     const float r = rsqrtf(sum * inv_dim + A.eps);
     const float back = -dot * inv_dim * r * r * r;  // dx = r w gu - x r^3 mean(w gu x)
     const uint64_t r2 = pack2(r, r), back2 = pack2(back, back);
-    if (h0 + at.step * groups < U.heads) {
+    const bool on = h0 + at.step * groups < U.heads;
+    if (on) {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const uint64_t ra = mul2(r2, ga[i]), rb = mul2(r2, gb[i]);
@@ -445,8 +508,9 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(NC * V)) backward_ke
         a[i] = fma2(ra, wa[i], mul2(a[i], back2));
         b[i] = fma2(rb, wb[i], mul2(b[i], back2));
       }
-      mine.store(to, a, b);
     }
+    mine.store(A, to, on, a, b, ring[warp][used][0]);
+    used = used + 1 == S ? 0 : used + 1;
     if (at.next(A, U))
       to = at.head<T>(Y, h0);
     else
@@ -469,9 +533,9 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(NC * V)) backward_ke
       va += __shfl_xor_sync(0xffffffffu, va, o);
       vb += __shfl_xor_sync(0xffffffffu, vb, o);
     }
-    if (lane < A.group && mine.has[i / V]) {
+    if (lane < A.group && mine.has[i / L::kWidth]) {
       int place, apart;
-      pair_place<INTER>(L::first_pair(A, i / V) + i % V, A.dim, A.half, place, apart);
+      pair_place<L::INTER>(L::first_pair(A, i / L::kWidth) + i % L::kWidth, A.dim, A.half, place, apart);
       red[warp * 2 * kMaxPairs + place] = va, red[warp * 2 * kMaxPairs + place + apart] = vb;
     }
   }
@@ -538,14 +602,12 @@ dion_status check_shape(const dion_qknorm_plan *p, const dion_qk_shape *s) {
   if (s->heads > kMaxHeads || s->kv_heads > kMaxHeads) return DION_ERR_UNSUPPORTED;
   if (s->positions && !aligned_to(s->positions, s->position_dtype == DION_INDEX_INT64 ? 8 : 4)) return DION_ERR_ALIGNMENT;
   if (s->batch > 0 && s->tokens > INT32_MAX / s->batch) return DION_ERR_UNSUPPORTED;
-  const int64_t limit = (int64_t)1 << 40, per = ((int64_t)s->heads + s->kv_heads) * p->head_dim;
-  if (s->batch > 0 && s->tokens > 0 && (per > limit || s->batch > limit / per || s->tokens > limit / per / s->batch))
-    return DION_ERR_UNSUPPORTED;
   return DION_OK;
 }
 
-// Args of a call whose kernel has `blocks` resident blocks, and the blocks that it takes.
-Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int v, int nc, int64_t resident, int64_t *blocks) {
+// Args of a call whose kernel has `pairs` pairs per lane and `resident` blocks at a time, and the blocks that it
+// takes.
+Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int pairs, int64_t resident, int64_t *blocks) {
   Args A{};
   A.tokens = (int32_t)s->tokens, A.all = (int32_t)(s->batch * s->tokens);
   A.hq = s->heads, A.hk = s->kv_heads;
@@ -553,7 +615,7 @@ Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int v, int nc,
   A.pos = s->positions, A.pos_sb = s->position_batch_stride, A.pos_dtype = s->position_dtype;
   A.turn = p->turn;
   A.group = 1;
-  while (A.group * nc * v < p->head_dim / 2) A.group *= 2;
+  while (A.group * pairs < p->head_dim / 2) A.group *= 2;
   const int groups = 32 / A.group;
   A.q_steps = (A.hq + groups - 1) / groups, A.k_steps = (A.hk + groups - 1) / groups;
   const int64_t cycle = A.q_steps + A.k_steps, work = A.all * cycle;
@@ -563,20 +625,36 @@ Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int v, int nc,
   return A;
 }
 
+// Whether every head of the tensors is whole 16-byte pieces.
+bool heads_in_pieces(const dion_qknorm_plan *p, const dion_qk_shape *s, const Heads *h, int n) {
+  const int es = element_bytes(s->dtype), v = 16 / es;
+  bool fits = p->head_dim % v == 0;
+  for (int i = 0; i < n; ++i)
+    fits = fits && (!h[i].p || (aligned_to(h[i].p, 16) && h[i].sb % v == 0 && h[i].st % v == 0 && h[i].sh % v == 0));
+  return fits;
+}
+
+// What a lane holds: `v` pairs per access, or staged.
+template <class L>
+struct Tag {
+  using type = L;
+};
 template <class T, bool INTER, class F>
-cudaError_t with_width(int v, F &&f) {
+cudaError_t with_width(int v, bool staged, F &&f) {
   if constexpr (sizeof(T) == 2)
-    if (v == 8) return f(T(), std::integral_constant<int, 8>(), std::integral_constant<int, 1>(), std::integral_constant<bool, INTER>());
-  if (v == 4) return f(T(), std::integral_constant<int, 4>(), std::integral_constant<int, 1>(), std::integral_constant<bool, INTER>());
-  if (v == 2) return f(T(), std::integral_constant<int, 2>(), std::integral_constant<int, 2>(), std::integral_constant<bool, INTER>());
-  return f(T(), std::integral_constant<int, 1>(), std::integral_constant<int, 4>(), std::integral_constant<bool, INTER>());
+    if (v == 8) return f(Tag<Lane<T, 8, 1, INTER>>());
+  if (v == 4) return f(Tag<Lane<T, 4, 1, INTER>>());
+  if constexpr (!INTER)
+    if (staged) return f(Tag<StagedLane<T>>());
+  if (v == 2) return f(Tag<Lane<T, 2, 2, INTER>>());
+  return f(Tag<Lane<T, 1, 4, INTER>>());
 }
 template <class F>
-cudaError_t with_kernel(int32_t dtype, int v, bool inter, F &&f) {
-  if (dtype == DION_DTYPE_FP32) return inter ? with_width<float, true>(v, f) : with_width<float, false>(v, f);
-  return inter ? with_width<__nv_bfloat16, true>(v, f) : with_width<__nv_bfloat16, false>(v, f);
+cudaError_t with_lane(int32_t dtype, int v, bool staged, bool inter, F &&f) {
+  using BF = __nv_bfloat16;
+  if (dtype == DION_DTYPE_FP32) return inter ? with_width<float, true>(v, staged, f) : with_width<float, false>(v, staged, f);
+  return inter ? with_width<BF, true>(v, staged, f) : with_width<BF, false>(v, staged, f);
 }
-int chunks_per_lane(int v) { return v >= 4 ? 1 : 4 / v; }
 
 }  // namespace
 
@@ -643,11 +721,10 @@ dion_status dion_qknorm_forward(dion_qknorm_plan *p, const dion_qk_shape *s, con
                       heads_of(s->heads ? q_out : nullptr), heads_of(s->kv_heads ? k_out : nullptr)};
   const int v = pair_width(p, s, h, 4);
   int64_t blocks = 0;
-  Args A = make_args(p, s, v, chunks_per_lane(v), (int64_t)p->num_sms * forward_blocks(chunks_per_lane(v) * v), &blocks);
+  Args A = make_args(p, s, v == 8 ? 8 : 4, (int64_t)p->num_sms * forward_blocks(v == 8 ? 8 : 4), &blocks);
   A.q = h[0], A.k = h[1], A.oq = h[2], A.ok = h[3], A.wq = wq, A.wk = wk;
-  const cudaError_t e = with_kernel(s->dtype, v, p->interleaved, [&](auto t, auto V, auto NC, auto I) {
-    return launch(forward_kernel<decltype(t), decltype(V)::value, decltype(NC)::value, decltype(I)::value>, blocks, kThreads,
-                  0, static_cast<cudaStream_t>(stream), 1, A);
+  const cudaError_t e = with_lane(s->dtype, v, heads_in_pieces(p, s, h, 4), p->interleaved, [&](auto lane) {
+    return launch(forward_kernel<typename decltype(lane)::type>, blocks, kThreads, 0, static_cast<cudaStream_t>(stream), 1, A);
   });
   return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
 }
@@ -676,12 +753,11 @@ dion_status dion_qknorm_backward(dion_qknorm_plan *p, const dion_qk_shape *s, co
   }
   const int v = pair_width(p, s, h, 6);
   int64_t blocks = 0;
-  Args A = make_args(p, s, v, chunks_per_lane(v), (int64_t)p->num_sms * backward_blocks(chunks_per_lane(v) * v), &blocks);
+  Args A = make_args(p, s, v == 8 ? 8 : 4, (int64_t)p->num_sms * backward_blocks(v == 8 ? 8 : 4), &blocks);
   A.gq = h[0], A.gk = h[1], A.q = h[2], A.k = h[3], A.oq = h[4], A.ok = h[5];
   A.wq = wq, A.wk = wk, A.partial = dwq || dwk ? p->partial : nullptr;
-  cudaError_t e = with_kernel(s->dtype, v, p->interleaved, [&](auto t, auto V, auto NC, auto I) {
-    return launch(backward_kernel<decltype(t), decltype(V)::value, decltype(NC)::value, decltype(I)::value>, blocks, kThreads,
-                  0, cs, 1, A);
+  cudaError_t e = with_lane(s->dtype, v, heads_in_pieces(p, s, h, 6), p->interleaved, [&](auto lane) {
+    return launch(backward_kernel<typename decltype(lane)::type>, blocks, kThreads, 0, cs, 1, A);
   });
   if (e == cudaSuccess && A.partial)
     e = launch(sum_weights_kernel, (2 * p->head_dim + 31) / 32, kSumThreads, 0, cs, 1, p->partial, (int)blocks, p->head_dim, dwq,

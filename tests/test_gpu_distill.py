@@ -295,3 +295,22 @@ def test_packed_structs_follow_the_header():
         values = list(range(1, 1 + len(struct._fields_)))
         got = struct.from_buffer_copy(packed.pack(*values))
         assert [getattr(got, f[0]) for f in struct._fields_] == values
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(cd):
+    n, v = 43_000, 50_001  # 2.15e9 logits, odd rows
+    z = torch.zeros(n, v, dtype=BF16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    z[-5:] = (torch.randn(5, v, generator=g, device="cuda") * 3).to(BF16)
+    tail = z[-5:].clone()
+    ids = torch.randint(0, v, (n, 4), generator=g, device="cuda")
+    t = torch.randn(n, 4, generator=g, device="cuda")
+    w = torch.zeros(n, device="cuda")
+    w[-5:] = 1.0
+    loss, grad, loss_size, size = reference(tail, ids[-5:], t[-5:], 2.0, None, 0.0, w[-5:])
+    e = relative_error(tail, t[-5:], 2.0, 4)
+    l, gz = cd.distill_loss_grad(z, ids, t, 2.0, weights=w, out=(torch.empty(n, device="cuda"), z))  # in place
+    assert ((l[-5:].double() - loss).abs() <= e * loss_size).all() and not l[:-5].any()
+    assert ((gz[-5:].double() - grad).abs() <= 2 * e * size + OUT[BF16] * grad.abs()).all()
+    assert not gz[n // 2].any()

@@ -208,3 +208,24 @@ def test_c_refusals(cd):
     assert lib.dion_embed_lookup(None, p, 0, 1, p, 0, 4, 1.0, p, 0, 4, None) == n.DION_ERR_INVALID_ARG
     assert lib.dion_embed_gradient(None, p, 0, 1, p, 0, 4, 1.0, p, 0, 4, 0, None) == n.DION_ERR_INVALID_ARG
     lib.dion_embed_plan_destroy(None)
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(cd):
+    """A table of more than 2^31 elements, and more than 2^31 elements of activations."""
+    vocab, dim = 1_100_003, 2048
+    g = torch.Generator(device="cuda").manual_seed(6)
+    table = torch.empty(vocab, dim, dtype=BF16, device="cuda").normal_(generator=g)
+    tok = torch.cat([torch.tensor([vocab - 1, 0, vocab - 2, vocab - 1], device="cuda"),
+                     torch.randint(vocab // 2, vocab, (60,), generator=g, device="cuda")])
+    plan = cd.EmbedPlan(vocab, dim, 1_100_000)
+    assert torch.equal(plan.lookup(tok, table), table[tok])
+    many = torch.randint(0, vocab, (1_100_000,), generator=g, device="cuda")  # beyond one cluster's sort as well
+    out = plan.lookup(many, table)
+    last = slice(1_099_900, 1_100_000)
+    assert torch.equal(out[last], table[many[last]])
+    d = plan.gradient(many, out, out=table)  # bf16 in and out
+    for v in (int(many[-1]), int(many[0]), vocab - 1):
+        at = (many == v).nonzero()[:, 0]
+        want = out[at].double().sum(0)
+        assert ((d[v].double() - want).abs() <= want.abs() * 2.0 ** -8 + len(at) ** 2 * 2.0 ** -20).all()

@@ -247,3 +247,21 @@ def test_c_refusals(cd):
     assert lib.dion_qknorm_forward(None, sh, h, None, None, None, h, None, None) == n.DION_ERR_INVALID_ARG
     assert lib.dion_qknorm_backward(None, sh, h, None, h, None, None, None, h, None, None, None, None) == n.DION_ERR_INVALID_ARG
     lib.dion_qknorm_plan_destroy(None)
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(cd):
+    tokens, heads, d = 1_060_000, 16, 128  # 2.2e9 elements
+    q = torch.zeros(1, tokens, heads, d, dtype=BF16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    tail = torch.randn(1, 3, heads, d, generator=g, device="cuda").to(BF16)
+    q[:, -3:] = tail
+    plan = cd.QKNormPlan(d, eps=EPS)
+    y = plan.forward(q)[0]
+    want, size = forward_ref(tail, None, torch.arange(tokens - 3, tokens, device="cuda")[None], freq_of(d), False)
+    assert ((y[:, -3:].double() - want).abs() <= 40 * u * size + OUT[BF16] * want.abs()).all()
+    assert not y[:, tokens // 2].any()
+    dq = plan.backward(y, None, q, out=(y, None, None, None))[0]  # in place over the gradient
+    pos = torch.arange(tokens - 3, tokens, device="cuda")[None]
+    dx, dx_size, _, _ = backward_ref(plan.forward(tail, positions=pos)[0], tail, None, pos, freq_of(d), False)
+    assert ((dq[:, -3:].double() - dx).abs() <= 100 * u * dx_size + OUT[BF16] * dx.abs()).all()
