@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const 
 // --------------------------------------------------------------------------------- zero ---
 // Zeros in the rows that no token names.  A block has `rows` rows: it looks through all tokens for them, a
 // flag for each in shared memory, and then writes.  Runs beside the sort.
-constexpr int kZeroThreads = 512, kZeroMaxRows = 8192;
+constexpr int kZeroThreads = 1024, kZeroMaxRows = 8192;
 template <class T>
 __global__ void __launch_bounds__(kZeroThreads) zero_kernel(const void *tokens, int32_t dtype, int32_t n, int32_t vocab, int32_t dim,
                                                             int32_t rows, T *dst, int64_t ldd, int beside_sort) {
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kZeroThreads) zero_kernel(const void *tokens, 
     const int chunks = (dim - head) * (int)sizeof(T) / 16, rest = head + chunks * (16 / (int)sizeof(T));
     if (lane < head) row[lane] = T(0.f);
     uint4 *to = reinterpret_cast<uint4 *>(row + head);
-    for (int c = lane; c < chunks; c += 32) to[c] = make_uint4(0, 0, 0, 0);
+    for (int c = lane; c < chunks; c += 32) __stcs(to + c, make_uint4(0, 0, 0, 0));
     if (rest + lane < dim) row[rest + lane] = T(0.f);
   }
   if (beside_sort) chain_enter();
@@ -705,8 +705,8 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
   w.ldg = ldg, w.ldd = ldd, w.scale = scale;
   w.head = p->head, w.tail = p->tail, w.head_row = p->head_row, w.tail_row = p->tail_row;
   if (!accumulate) {
-    // two blocks on each SM that the sort leaves
-    const int64_t want = 2 * std::max(1, p->num_sms - kMaxClusterBlocks), rows = (p->vocab + want - 1) / want;
+    // a block on each SM that the sort leaves
+    const int64_t want = std::max(1, p->num_sms - kMaxClusterBlocks), rows = (p->vocab + want - 1) / want;
     const int32_t per = (int32_t)std::min<int64_t>(rows, kZeroMaxRows);
     const int64_t grid = (p->vocab + per - 1) / per;
     const int beside = num_tokens > 0;
