@@ -6,8 +6,9 @@
 //
 // A group of lanes holds a head as D / 2 pairs (the elements that pass are paired across their own
 // halves, with angle 0), so a rotation never leaves a lane; the mean is a shuffle sum over the group.
-// A warp keeps to one kind and a few of its heads and goes over tokens: it computes a token's sines and
-// cosines once, and holds the weights and the sums of their gradients in registers.  What it reads runs
+// A warp keeps to one kind and a few of its heads and goes over tokens (blocks of tokens, where the heads of
+// one do not fill a warp): it computes a token's sines and cosines once, and holds the weights and the
+// sums of their gradients in registers.  What it reads runs
 // ahead of it through a ring of asynchronous copies in shared memory, of which every lane reads only what
 // it copied itself.
 #include "lm_common.cuh"
@@ -16,6 +17,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <numeric>
 
 using namespace cd;
 using namespace cd::lm;
@@ -50,13 +52,35 @@ struct Heads {
   int64_t sb, st, sh;
 };
 
+// Division by a number that the host knows: n < 2^31 by d in a multiplication, an addition and a shift
+// (Granlund and Montgomery, 1994).
+struct FastDiv {
+  uint32_t d, m, l;
+  static FastDiv of(uint32_t d) {
+    uint32_t l = 0;
+    while (((uint64_t)1 << l) < d) ++l;
+    return {d, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1), l};
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) + n) >> l; }
+};
+
+constexpr int kMaxBlockTokens = 16;
+
+// q or k.  Head h of token j of a block is unit j heads + h; a step is as many units as a warp has groups.
+struct Kind {
+  int32_t heads, tokens;  // tokens of a block
+  int32_t steps, blocks;  // steps of a block, blocks in all
+  int32_t weight;         // warps that a step counts for, among those of both kinds
+  FastDiv by_heads;
+};
+
 struct Args {
-  int32_t tokens, all;  // of a sequence, of all
-  int32_t hq, hk;
-  int32_t q_steps, k_steps;  // of a token: a head for each group of a warp's lanes
-  int32_t steps;             // of these, what a warp takes (a batch) at most
-  int32_t dim, half;           // half = rotary / 2
-  int32_t group;               // lanes per head
+  int32_t all;  // tokens of all sequences
+  FastDiv by_tokens, by_pairs;
+  Kind kind[2];
+  int32_t steps;      // of a block, what a warp takes (a batch) at most
+  int32_t dim, half;  // half = rotary / 2
+  int32_t group;      // lanes per head
   float eps;
   const void *pos;
   int64_t pos_sb;
@@ -88,6 +112,7 @@ struct Lane {
   using T = T_;
   static constexpr bool INTER = INTER_;
   static constexpr int kWidth = V, kPairs = NC * V, kPacks = kPairs / 2;
+  static constexpr int kAngles = kPairs * 32;  // of the tokens of a block: as many as the warp's lanes hold pairs
   static constexpr int kPiece = V * (int)sizeof(T);   // bytes
   static constexpr int kStep = 2 * NC * 32 * kPiece;  // of a warp's ring, a step of one tensor
   int at[NC], apart[NC];  // the pieces' first elements in a head: at, at + apart
@@ -250,22 +275,6 @@ __device__ __forceinline__ float group_sum(float v, int group) {
   return v;
 }
 
-// Sines and cosines of a token's pairs into the warp's shared memory.  position * turn wraps modulo one
-// turn exactly; the top 32 bits, as a signed fraction of half a turn, are within 2^-31 of it, and
-// fp32's rounding of that is 2^-25 of half a turn at most.
-__device__ __forceinline__ void token_angles(const Args &A, int64_t position, float *cs, float *sn) {
-  __syncwarp();  // the last token's were read
-  for (int u = threadIdx.x & 31; u < A.dim / 2; u += 32) {
-    float c = 1.f, s = 0.f;
-    if (u < A.half) {
-      const int32_t part = (int32_t)(((uint64_t)position * A.turn[u]) >> 32);
-      sincospif((float)part * 0x1p-31f, &s, &c);
-    }
-    cs[u] = c, sn[u] = s;
-  }
-  __syncwarp();
-}
-
 // The weights of both kinds by pairs, in shared memory: [kind][first or second of the pair][pair].
 template <bool INTER>
 __device__ __forceinline__ void stage_weights(const Args &A, float (&w)[2][2][kMaxPairs]) {
@@ -279,55 +288,91 @@ __device__ __forceinline__ void stage_weights(const Args &A, float (&w)[2][2][kM
   __syncthreads();
 }
 
-// What a warp goes over: a batch of one kind's heads, and every stride-th token.  A batch of n steps has n
-// of every q_steps + k_steps warps, so that all have the same work.
+// What a warp goes over: a batch of a kind's steps, and every stride-th block of tokens.  A batch of n steps
+// has n `weight` of every kind[0].steps kind[0].weight + kind[1].steps kind[1].weight warps, so that all have
+// the same work.
+// MULTI: whether blocks have several tokens.
+template <bool MULTI>
 struct Unit {
-  int kind, first_head, steps, heads, token, stride;
+  int kind, first_step, steps, heads, tokens, blocks, block, stride;
+  int groups, unit;  // of a step: its units, this lane's of the batch's first
+  FastDiv by_heads;
   __device__ __forceinline__ Unit(const Args &A, int id) {
-    const int cycle = A.q_steps + A.k_steps, slot = id % cycle;
-    kind = slot >= A.q_steps;
-    heads = kind ? A.hk : A.hq;
-    const int begin = kind ? A.q_steps : 0, in_kind = slot - begin, first_step = in_kind / A.steps * A.steps;
-    first_head = first_step * (32 / A.group);
-    steps = min(A.steps, (kind ? A.k_steps : A.q_steps) - first_step);
-    token = id / cycle * steps + in_kind - first_step;
-    const int warps = (int)gridDim.x * kWarps, left = warps % cycle - (begin + first_step);
-    stride = warps / cycle * steps + max(0, min(left, steps));
+    const int q_slots = A.kind[0].steps * A.kind[0].weight, cycle = q_slots + A.kind[1].steps * A.kind[1].weight;
+    const int slot = id % cycle;
+    kind = slot >= q_slots;
+    const Kind &K = A.kind[kind];
+    heads = K.heads, tokens = K.tokens, blocks = K.blocks, by_heads = K.by_heads;
+    const int begin = kind ? q_slots : 0, in_kind = slot - begin;
+    first_step = in_kind / K.weight / A.steps * A.steps;
+    steps = min(A.steps, K.steps - first_step);
+    groups = 32 / A.group, unit = first_step * groups + (threadIdx.x & 31) / A.group;
+    const int before = first_step * K.weight, share = steps * K.weight;
+    block = id / cycle * share + in_kind - before;
+    const int warps = (int)gridDim.x * kWarps, left = warps % cycle - begin - before;
+    stride = warps / cycle * share + max(0, min(left, share));
   }
 };
 
-// A token and a step of it; runs ahead of the work (the copies) or with it.
+// A block of tokens and a step of it, and this lane's head in it; runs ahead of the work (the copies) or
+// with it.
+template <bool MULTI>
 struct Cursor {
-  int token, step, seq, t;  // seq: tokens so far
-  int b;
-  __device__ __forceinline__ Cursor(const Args &A, const Unit &U) : token(U.token), step(0), seq(0) { place(A); }
-  __device__ __forceinline__ void place(const Args &A) {
-    b = (int)((unsigned)token / (unsigned)A.tokens);
-    t = token - b * A.tokens;
+  int block, step, seq;  // seq: blocks so far
+  int in_block, h;       // the head's token in the block, the head
+  int b, t;              // its sequence, its token there
+  bool real;
+  __device__ __forceinline__ Cursor(const Args &A, const Unit<MULTI> &U) : block(U.block), step(0), seq(0) { place(A, U); }
+  __device__ __forceinline__ void place(const Args &A, const Unit<MULTI> &U) {
+    const int unit = U.unit + step * U.groups;
+    in_block = MULTI ? (int)U.by_heads.div(unit) : 0;
+    h = unit - in_block * U.heads;
+    unsigned token = MULTI ? (unsigned)block * U.tokens + in_block : block;
+    real = h < U.heads;
+    if (MULTI) {
+      real = in_block < U.tokens && token < (unsigned)A.all;
+      if (!real) in_block = h = token = 0;
+    }
+    b = (int)A.by_tokens.div(token), t = (int)token - b * (int)A.by_tokens.d;
   }
-  __device__ __forceinline__ bool on(const Args &A) const { return token < A.all; }
-  // true where a new token begins
-  __device__ __forceinline__ bool next(const Args &A, const Unit &U) {
-    if (++step < U.steps) return false;
+  __device__ __forceinline__ bool on(const Unit<MULTI> &U) const { return block < U.blocks; }
+  // the next step; true where the head is no longer in the same token
+  __device__ __forceinline__ bool next(const Args &A, const Unit<MULTI> &U) {
+    if (++step < U.steps) {
+      if (MULTI) {
+        place(A, U);
+        return true;
+      }
+      h += U.groups;
+      real = h < U.heads;
+      return false;
+    }
     step = 0, ++seq;
-    token = U.stride < A.all - token ? token + U.stride : A.all;
-    if (token < A.all) place(A);
+    block = U.stride < U.blocks - block ? block + U.stride : U.blocks;
+    if (block < U.blocks) place(A, U);
     return true;
   }
   template <class T>
-  __device__ __forceinline__ T *head(const Heads &H, int h) const {
+  __device__ __forceinline__ T *head(const Heads &H) const {
     return static_cast<T *>(H.p) + b * H.sb + t * H.st + h * H.sh;
   }
 };
 
-// The positions of the tokens on their way: lane 0 copies a token's with its first step.
-template <int S>
+// The positions of the blocks on their way: a lane per token copies them with the block's first step.
+template <int S, bool MULTI>
 struct Positions {
-  int64_t slot[S];
-  __device__ __forceinline__ void copy(const Args &A, const Cursor &c) {
-    if (!A.pos || c.step != 0 || (threadIdx.x & 31) != 0) return;
-    int64_t *to = &slot[c.seq % S];
-    const int64_t i = (int64_t)c.b * A.pos_sb + c.t;
+  int64_t slot[S][MULTI ? kMaxBlockTokens : 1];
+  __device__ __forceinline__ void copy(const Args &A, const Unit<MULTI> &U, const Cursor<MULTI> &c) {
+    const int lane = threadIdx.x & 31;
+    if (!A.pos || c.step != 0 || lane >= (MULTI ? U.tokens : 1)) return;
+    int b = c.b, t = c.t;
+    if (MULTI) {
+      const unsigned token = (unsigned)c.block * U.tokens + lane;
+      if (token >= (unsigned)A.all) return;
+      b = (int)A.by_tokens.div(token), t = (int)token - b * (int)A.by_tokens.d;
+    }
+    int64_t *to = &slot[c.seq % S][lane];
+    const int64_t i = b * A.pos_sb + t;
     if (A.pos_dtype == DION_INDEX_INT64)
       asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(tc::smem_u32(to)), "l"(static_cast<const int64_t *>(A.pos) + i)
                    : "memory");
@@ -335,12 +380,34 @@ struct Positions {
       asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::smem_u32(to)), "l"(static_cast<const int32_t *>(A.pos) + i)
                    : "memory");
   }
-  // after the copies are complete for lane 0, and a __syncwarp
-  __device__ __forceinline__ int64_t of(const Args &A, const Cursor &c) const {
-    const int64_t *from = &slot[c.seq % S];
-    return !A.pos ? c.t : A.pos_dtype == DION_INDEX_INT64 ? *from : (int64_t)*reinterpret_cast<const int32_t *>(from);
+  __device__ __forceinline__ int64_t of(const Args &A, int seq, int in_block) const {
+    const int64_t *from = &slot[seq % S][in_block];
+    return A.pos_dtype == DION_INDEX_INT64 ? *from : (int64_t)*reinterpret_cast<const int32_t *>(from);
   }
 };
+
+// Sines and cosines of the pairs of a block's tokens into the warp's shared memory, [token][pair].  position *
+// turn wraps modulo one turn exactly; the top 32 bits, as a signed fraction of half a turn, are within
+// 2^-31 of it, and fp32's rounding of that is 2^-25 of half a turn at most.
+template <int S, bool MULTI>
+__device__ __forceinline__ void block_angles(const Args &A, const Unit<MULTI> &U, const Cursor<MULTI> &at,
+                                             const Positions<S, MULTI> &positions, float *cs, float *sn) {
+  __syncwarp();  // the last block's were read; this one's positions are there for every lane
+  const int pairs = A.dim / 2;
+  const int64_t only = MULTI ? 0 : A.pos ? positions.of(A, at.seq, 0) : at.t;
+  for (int i = threadIdx.x & 31; i < (MULTI ? U.tokens : 1) * pairs; i += 32) {
+    const int j = MULTI ? (int)A.by_pairs.div(i) : 0, u = i - j * pairs;
+    const unsigned token = MULTI ? (unsigned)at.block * U.tokens + j : at.block;
+    float c = 1.f, s = 0.f;
+    if (u < A.half && token < (unsigned)A.all) {
+      const int64_t position = !MULTI ? only : A.pos ? positions.of(A, at.seq, j) : token - A.by_tokens.div(token) * A.by_tokens.d;
+      const int32_t part = (int32_t)(((uint64_t)position * A.turn[u]) >> 32);
+      sincospif((float)part * 0x1p-31f, &s, &c);
+    }
+    cs[i] = c, sn[i] = s;
+  }
+  __syncwarp();
+}
 
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -349,30 +416,29 @@ __device__ __forceinline__ void wait_copies() {
 }
 
 // ------------------------------------------------------------------------------ forward ---
-template <class L>
+template <class L, bool MULTI>
 __global__ void __launch_bounds__(kThreads, forward_blocks(L::kPairs)) forward_kernel(const __grid_constant__ Args A) {
   using T = typename L::T;
   constexpr int S = kRing, P = L::kPacks;
-  __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs];
+  __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][MULTI ? L::kAngles : kMaxPairs];
   __shared__ __align__(16) char ring[kWarps][S][L::kStep];
-  __shared__ Positions<S> positions[kWarps];
+  __shared__ Positions<S, MULTI> positions[kWarps];
   chain_enter();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = 32 / A.group;
-  const Unit U(A, blockIdx.x * kWarps + warp);
+  const int warp = threadIdx.x >> 5;
+  const Unit<MULTI> U(A, blockIdx.x * kWarps + warp);
   const Heads &X = U.kind ? A.k : A.q, &Y = U.kind ? A.ok : A.oq;
   const L mine(A);
-  const int h0 = U.first_head + lane / A.group;
-  const int64_t x_step = groups * X.sh, y_step = groups * Y.sh;
-  Cursor ahead(A, U), at(A, U);
-  const T *from = ahead.head<const T>(X, h0);
-  T *to = at.head<T>(Y, h0);
+  const int64_t x_step = U.groups * X.sh, y_step = U.groups * Y.sh;
+  Cursor<MULTI> ahead(A, U), at(A, U);
+  const T *from = ahead.template head<const T>(X);
+  T *to = at.template head<T>(Y);
   int filled = 0, used = 0;  // places of the ring
   auto fill = [&] {
-    if (ahead.on(A)) {
-      mine.copy(A, from, h0 + ahead.step * groups < U.heads, ring[warp][filled]);
-      positions[warp].copy(A, ahead);
+    if (ahead.on(U)) {
+      mine.copy(A, from, ahead.real, ring[warp][filled]);
+      positions[warp].copy(A, U, ahead);
       if (ahead.next(A, U))
-        from = ahead.head<const T>(X, h0);
+        from = ahead.template head<const T>(X);
       else
         from += x_step;
     }
@@ -384,14 +450,14 @@ __global__ void __launch_bounds__(kThreads, forward_blocks(L::kPairs)) forward_k
   stage_weights<L::INTER>(A, w);  // while the first steps are on their way
   const float inv_dim = 1.f / (float)A.dim;
   uint64_t ac[P], bs[P], bc[P], as[P];  // of a token: wa cos, -wb sin, wb cos, wa sin
-  while (at.on(A)) {
+  while (at.on(U)) {
     wait_copies<S - 2>();
-    if (at.step == 0) {
-      __syncwarp();
-      token_angles(A, positions[warp].of(A, at), angles[warp][0], angles[warp][1]);
+    if (at.step == 0) block_angles(A, U, at, positions[warp], angles[warp][0], angles[warp][1]);
+    if (at.step == 0 || MULTI) {
+      const int first = at.in_block * (A.dim / 2);
       uint64_t c[P], s[P], wa[P], wb[P];
-      mine.read_pairs(angles[warp][0], A, c);
-      mine.read_pairs(angles[warp][1], A, s);
+      mine.read_pairs(angles[warp][0] + first, A, c);
+      mine.read_pairs(angles[warp][1] + first, A, s);
       mine.read_pairs(w[U.kind][0], A, wa);
       mine.read_pairs(w[U.kind][1], A, wb);
 #pragma unroll
@@ -414,10 +480,10 @@ __global__ void __launch_bounds__(kThreads, forward_blocks(L::kPairs)) forward_k
       ya[i] = mul2(r2, fma2(b[i], bs[i], mul2(a[i], ac[i])));
       yb[i] = mul2(r2, fma2(a[i], as[i], mul2(b[i], bc[i])));
     }
-    mine.store(A, to, h0 + at.step * groups < U.heads, ya, yb, ring[warp][used]);
+    mine.store(A, to, at.real, ya, yb, ring[warp][used]);
     used = used + 1 == S ? 0 : used + 1;
     if (at.next(A, U))
-      to = at.head<T>(Y, h0);
+      to = at.template head<T>(Y);
     else
       to += y_step;
     fill();
@@ -425,32 +491,30 @@ __global__ void __launch_bounds__(kThreads, forward_blocks(L::kPairs)) forward_k
 }
 
 // ----------------------------------------------------------------------------- backward ---
-template <class L>
+template <class L, bool MULTI>
 __global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward_kernel(const __grid_constant__ Args A) {
   using T = typename L::T;
   constexpr int S = kRing, P = L::kPacks;
-  __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][kMaxPairs];
+  __shared__ __align__(16) float w[2][2][kMaxPairs], angles[kWarps][2][MULTI ? L::kAngles : kMaxPairs];
   __shared__ __align__(16) char ring[kWarps][S][2][L::kStep];
-  __shared__ Positions<S> positions[kWarps];
+  __shared__ Positions<S, MULTI> positions[kWarps];
   chain_enter();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = 32 / A.group;
-  const Unit U(A, blockIdx.x * kWarps + warp);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Unit<MULTI> U(A, blockIdx.x * kWarps + warp);
   const Heads &X = U.kind ? A.k : A.q, &G = U.kind ? A.gk : A.gq, &Y = U.kind ? A.ok : A.oq;
   const L mine(A);
-  const int h0 = U.first_head + lane / A.group;
-  const int64_t x_step = groups * X.sh, g_step = groups * G.sh, y_step = groups * Y.sh;
-  Cursor ahead(A, U), at(A, U);
-  const T *from = ahead.head<const T>(X, h0), *from_g = ahead.head<const T>(G, h0);
-  T *to = at.head<T>(Y, h0);
+  const int64_t x_step = U.groups * X.sh, g_step = U.groups * G.sh, y_step = U.groups * Y.sh;
+  Cursor<MULTI> ahead(A, U), at(A, U);
+  const T *from = ahead.template head<const T>(X), *from_g = ahead.template head<const T>(G);
+  T *to = at.template head<T>(Y);
   int filled = 0, used = 0;
   auto fill = [&] {
-    if (ahead.on(A)) {
-      const bool on = h0 + ahead.step * groups < U.heads;
-      mine.copy(A, from, on, ring[warp][filled][0]);
-      mine.copy(A, from_g, on, ring[warp][filled][1]);
-      positions[warp].copy(A, ahead);
+    if (ahead.on(U)) {
+      mine.copy(A, from, ahead.real, ring[warp][filled][0]);
+      mine.copy(A, from_g, ahead.real, ring[warp][filled][1]);
+      positions[warp].copy(A, U, ahead);
       if (ahead.next(A, U))
-        from = ahead.head<const T>(X, h0), from_g = ahead.head<const T>(G, h0);
+        from = ahead.template head<const T>(X), from_g = ahead.template head<const T>(G);
       else
         from += x_step, from_g += g_step;
     }
@@ -466,13 +530,13 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward
   mine.read_pairs(w[U.kind][1], A, wb);
 #pragma unroll
   for (int i = 0; i < P; ++i) da[i] = db[i] = 0;
-  while (at.on(A)) {
+  while (at.on(U)) {
     wait_copies<S - 2>();
-    if (at.step == 0) {
-      __syncwarp();
-      token_angles(A, positions[warp].of(A, at), angles[warp][0], angles[warp][1]);
-      mine.read_pairs(angles[warp][0], A, c);
-      mine.read_pairs(angles[warp][1], A, s);
+    if (at.step == 0) block_angles(A, U, at, positions[warp], angles[warp][0], angles[warp][1]);
+    if (at.step == 0 || MULTI) {
+      const int first = at.in_block * (A.dim / 2);
+      mine.read_pairs(angles[warp][0] + first, A, c);
+      mine.read_pairs(angles[warp][1] + first, A, s);
 #pragma unroll
       for (int i = 0; i < P; ++i) ns[i] = mul2(s[i], pack2(-1.f, -1.f));
     }
@@ -499,8 +563,7 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward
     const float r = rsqrtf(sum * inv_dim + A.eps);
     const float back = -dot * inv_dim * r * r * r;  // dx = r w gu - x r^3 mean(w gu x)
     const uint64_t r2 = pack2(r, r), back2 = pack2(back, back);
-    const bool on = h0 + at.step * groups < U.heads;
-    if (on) {
+    if (at.real) {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const uint64_t ra = mul2(r2, ga[i]), rb = mul2(r2, gb[i]);
@@ -509,10 +572,10 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward
         b[i] = fma2(rb, wb[i], mul2(b[i], back2));
       }
     }
-    mine.store(A, to, on, a, b, ring[warp][used][0]);
+    mine.store(A, to, at.real, a, b, ring[warp][used][0]);
     used = used + 1 == S ? 0 : used + 1;
     if (at.next(A, U))
-      to = at.head<T>(Y, h0);
+      to = at.template head<T>(Y);
     else
       to += y_step;
     fill();
@@ -520,8 +583,9 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward
   if (!A.partial) return;
   // the block's sums of dw, over the groups of a warp, then over the warps, in the angles' place
   __syncwarp();
+  constexpr int kRed = sizeof(angles[0]) / sizeof(float);
   float *red = &angles[0][0][0];  // [kWarps][dim] of the warp's kind
-  for (int d = lane; d < A.dim; d += 32) red[warp * 2 * kMaxPairs + d] = 0.f;
+  for (int d = lane; d < A.dim; d += 32) red[warp * kRed + d] = 0.f;
   __syncwarp();
 #pragma unroll
   for (int i = 0; i < L::kPairs; ++i) {
@@ -536,15 +600,16 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward
     if (lane < A.group && mine.has[i / L::kWidth]) {
       int place, apart;
       pair_place<L::INTER>(L::first_pair(A, i / L::kWidth) + i % L::kWidth, A.dim, A.half, place, apart);
-      red[warp * 2 * kMaxPairs + place] = va, red[warp * 2 * kMaxPairs + place + apart] = vb;
+      red[warp * kRed + place] = va, red[warp * kRed + place + apart] = vb;
     }
   }
   __syncthreads();
+  const int q_slots = A.kind[0].steps * A.kind[0].weight, cycle = q_slots + A.kind[1].steps * A.kind[1].weight;
   for (int d = threadIdx.x; d < 2 * A.dim; d += kThreads) {
     const int kind = d >= A.dim;
     float v = 0.f;
     for (int k = 0; k < kWarps; ++k)
-      if ((((int)blockIdx.x * kWarps + k) % (A.q_steps + A.k_steps) >= A.q_steps) == (kind != 0)) v += red[k * 2 * kMaxPairs + d - kind * A.dim];
+      if ((((int)blockIdx.x * kWarps + k) % cycle >= q_slots) == (kind != 0)) v += red[k * kRed + d - kind * A.dim];
     A.partial[(int64_t)blockIdx.x * 2 * A.dim + d] = v;
   }
 }
@@ -605,21 +670,49 @@ dion_status check_shape(const dion_qknorm_plan *p, const dion_qk_shape *s) {
   return DION_OK;
 }
 
+// Tokens of a block for `heads` heads of which a warp takes `groups` at a time: the number with the least
+// instructions per token, of about 170 for a step (300 where each step is of other tokens), 50 for each 32 of
+// the block's angles, 80 for the block.  Blocks of several tokens leave every warp one at least.  (71829
+// tokens of 3 + 3 heads of 96 in bf16: 91 us token by token, 68 in blocks of four; 63915 tokens of 12 + 3 heads
+// of 32: 67 and 38 us.)
+int block_tokens(int heads, int groups, int pairs, int most, int64_t all, int64_t warps) {
+  auto cost = [&](int n) {
+    const int steps = (n * heads + groups - 1) / groups;
+    return (double)(steps * (n > 1 ? 300 : 170) + (n * pairs + 31) / 32 * 50 + 80) / n;
+  };
+  int best = 1;
+  for (int n = 2; heads > 0 && n <= most && (all + n - 1) / n >= warps; ++n)
+    if (cost(n) < cost(best)) best = n;
+  return best;
+}
+
 // Args of a call whose kernel has `pairs` pairs per lane and `resident` blocks at a time, and the blocks that it
 // takes.
 Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int pairs, int64_t resident, int64_t *blocks) {
   Args A{};
-  A.tokens = (int32_t)s->tokens, A.all = (int32_t)(s->batch * s->tokens);
-  A.hq = s->heads, A.hk = s->kv_heads;
+  A.all = (int32_t)(s->batch * s->tokens);
+  A.by_tokens = FastDiv::of((uint32_t)s->tokens), A.by_pairs = FastDiv::of((uint32_t)p->head_dim / 2);
   A.dim = p->head_dim, A.half = p->rotary / 2, A.eps = p->eps;
   A.pos = s->positions, A.pos_sb = s->position_batch_stride, A.pos_dtype = s->position_dtype;
   A.turn = p->turn;
   A.group = 1;
   while (A.group * pairs < p->head_dim / 2) A.group *= 2;
-  const int groups = 32 / A.group;
-  A.q_steps = (A.hq + groups - 1) / groups, A.k_steps = (A.hk + groups - 1) / groups;
-  const int64_t cycle = A.q_steps + A.k_steps, work = A.all * cycle;
-  // a warp takes several steps of a token, which share its angles, as far as every warp has some
+  const int groups = 32 / A.group, most = std::min(kMaxBlockTokens, pairs * 64 / p->head_dim);
+  int64_t cycle = 0, work = 0;
+  for (int i = 0; i < 2; ++i) {
+    Kind &K = A.kind[i];
+    K.heads = i ? s->kv_heads : s->heads;
+    K.tokens = block_tokens(K.heads, groups, p->head_dim / 2, most, A.all, resident * kWarps);
+    K.steps = (K.tokens * K.heads + groups - 1) / groups;
+    K.blocks = (int32_t)(((int64_t)A.all + K.tokens - 1) / K.tokens);
+    K.by_heads = FastDiv::of((uint32_t)std::max(K.heads, 1));
+  }
+  for (int i = 0; i < 2; ++i) {  // a step of this kind is done once for each of its blocks
+    Kind &K = A.kind[i];
+    K.weight = A.kind[1 - i].tokens / std::gcd(K.tokens, A.kind[1 - i].tokens);
+    cycle += (int64_t)K.steps * K.weight, work += (int64_t)K.steps * K.blocks;
+  }
+  // a warp takes several steps of a block, which share its angles, as far as every warp has some
   A.steps = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kMaxSteps, work / (resident * kWarps)));
   *blocks = (std::max(std::min(resident * kWarps, work), cycle) + kWarps - 1) / kWarps;
   return A;
@@ -682,8 +775,8 @@ dion_status dion_qknorm_plan_create(int32_t head_dim, int32_t rotary_dim, int32_
   p->head_dim = head_dim, p->rotary = rotary_dim, p->interleaved = interleaved != 0, p->eps = eps;
   cudaError_t e = cudaGetDevice(&p->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->num_sms, cudaDevAttrMultiProcessorCount, p->device);
-  // the resident blocks, or a warp for every batch of the most heads that a call may have
-  p->max_blocks = std::max<int64_t>((int64_t)p->num_sms * backward_blocks(4), 2 * kMaxHeads / kWarps);
+  // the resident blocks, or a warp for every step (times its weight) of the most heads that a call may have
+  p->max_blocks = std::max<int64_t>((int64_t)p->num_sms * backward_blocks(4), 4 * kMaxHeads / kWarps);
   const size_t o_partial = sizeof(turn);
   if (e == cudaSuccess) e = cudaMalloc(&p->ws, o_partial + sizeof(float) * 2 * head_dim * p->max_blocks);
   if (e == cudaSuccess) {
@@ -723,8 +816,11 @@ dion_status dion_qknorm_forward(dion_qknorm_plan *p, const dion_qk_shape *s, con
   int64_t blocks = 0;
   Args A = make_args(p, s, v == 8 ? 8 : 4, (int64_t)p->num_sms * forward_blocks(v == 8 ? 8 : 4), &blocks);
   A.q = h[0], A.k = h[1], A.oq = h[2], A.ok = h[3], A.wq = wq, A.wk = wk;
+  const bool multi = A.kind[0].tokens > 1 || A.kind[1].tokens > 1;
   const cudaError_t e = with_lane(s->dtype, v, heads_in_pieces(p, s, h, 4), p->interleaved, [&](auto lane) {
-    return launch(forward_kernel<typename decltype(lane)::type>, blocks, kThreads, 0, static_cast<cudaStream_t>(stream), 1, A);
+    using L = typename decltype(lane)::type;
+    return launch(multi ? forward_kernel<L, true> : forward_kernel<L, false>, blocks, kThreads, 0,
+                  static_cast<cudaStream_t>(stream), 1, A);
   });
   return e == cudaSuccess ? DION_OK : DION_ERR_CUDA;
 }
@@ -756,8 +852,10 @@ dion_status dion_qknorm_backward(dion_qknorm_plan *p, const dion_qk_shape *s, co
   Args A = make_args(p, s, v == 8 ? 8 : 4, (int64_t)p->num_sms * backward_blocks(v == 8 ? 8 : 4), &blocks);
   A.gq = h[0], A.gk = h[1], A.q = h[2], A.k = h[3], A.oq = h[4], A.ok = h[5];
   A.wq = wq, A.wk = wk, A.partial = dwq || dwk ? p->partial : nullptr;
+  const bool multi = A.kind[0].tokens > 1 || A.kind[1].tokens > 1;
   cudaError_t e = with_lane(s->dtype, v, heads_in_pieces(p, s, h, 6), p->interleaved, [&](auto lane) {
-    return launch(backward_kernel<typename decltype(lane)::type>, blocks, kThreads, 0, cs, 1, A);
+    using L = typename decltype(lane)::type;
+    return launch(multi ? backward_kernel<L, true> : backward_kernel<L, false>, blocks, kThreads, 0, cs, 1, A);
   });
   if (e == cudaSuccess && A.partial)
     e = launch(sum_weights_kernel, (2 * p->head_dim + 31) / 32, kSumThreads, 0, cs, 1, p->partial, (int)blocks, p->head_dim, dwq,
