@@ -130,6 +130,39 @@ def test_forward_and_backward(cd, b, t, hq, hk, d, rot, inter, layout, weights, 
     assert torch.equal(gq, grads[0]) and (gk is None or torch.equal(gk, grads[1]))
 
 
+MANY = [  # batch, tokens, heads, kv_heads, head_dim, rotary, interleaved, layout: many tokens with few heads
+    (37, 811, 3, 3, 96, 96, False, "plain"), (40001, 1, 1, 1, 64, 64, False, "packed"), (3, 9999, 5, 1, 80, 32, False, "packed"),
+    (1, 30011, 2, 0, 32, 16, True, "heads_first"), (9001, 7, 12, 3, 32, 32, False, "plain"), (5003, 3, 1, 2, 256, 102, False, "plain"),
+    (101, 301, 3, 1, 20, 12, True, "odd"), (2, 15013, 1, 3, 128, 128, False, "odd"), (129, 257, 2, 1, 36, 0, False, "heads_first"),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("b,t,hq,hk,d,rot,inter,layout", MANY)
+def test_many_tokens_of_few_heads(cd, b, t, hq, hk, d, rot, inter, layout, dtype):
+    """Sequences that end anywhere, default positions and one row of them; queries and keys with their own blocks."""
+    g = torch.Generator(device="cuda").manual_seed(d + t)
+    q, k = make((b, t, hq, d), dtype, layout, g), make((b, t, hk, d), dtype, layout, g) if hk else None
+    gq, gk = make(q.shape, dtype, "plain", g), make(k.shape, dtype, layout, g) if hk else None
+    wq, wk = (torch.randn(d, generator=g, device="cuda") for _ in "qk")
+    row = torch.randint(-1000, 1 << 20, (t,), generator=g, device="cuda", dtype=torch.int32)
+    each = torch.randint(-1000, 1 << 20, (b, t), generator=g, device="cuda")
+    freq = freq_of(rot)
+    plan = cd.QKNormPlan(d, rot, interleaved=inter, eps=EPS)
+    for pos, given in ((torch.arange(t, device="cuda")[None], None), (row[None], row), (each, each)):
+        outs = plan.forward(q, k, wq, wk, given)
+        grads = plan.backward(gq, gk, q, k, wq, wk, given)
+        for i, (x, gx, w) in enumerate(((q, gq, wq), (k, gk, wk))):
+            if x is None:
+                continue
+            want, size = forward_ref(x, w, pos, freq, inter)  # bounds as above
+            assert ((outs[i].double() - want).abs() <= 40 * u * size + OUT[dtype] * want.abs()).all()
+            dx, dx_size, dw, dw_tol = backward_ref(gx, x, w, pos, freq, inter)
+            assert ((grads[i].double() - dx).abs() <= 100 * u * dx_size + OUT[dtype] * dx.abs()).all()
+            assert ((grads[2 + i].double() - dw).abs() <= dw_tol).all()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("index", [torch.int32, torch.int64])
 def test_positions(cd, index):
