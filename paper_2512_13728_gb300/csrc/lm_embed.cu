@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 using namespace cd;
 using namespace cd::lm;
@@ -233,10 +234,8 @@ __device__ __forceinline__ void store_cluster(uint2 *p, uint32_t rank, uint2 v) 
 }
 
 template <int I>
-__global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const void *tokens, int32_t dtype, int64_t vocab,
-                                                                          int32_t n, int passes, int bits, int blocks,
-                                                                          uint2 *out) {
-  extern __shared__ __align__(16) char sort_mem[];
+__device__ __forceinline__ void cluster_sort(char *sort_mem, const void *tokens, int32_t dtype, int64_t vocab, int32_t n,
+                                             int passes, int bits, int blocks, uint2 *out) {
   uint16_t(*count)[kMaxBins] = reinterpret_cast<uint16_t(*)[kMaxBins]>(sort_mem);  // [warp][digit]
   uint2 *entry = reinterpret_cast<uint2 *>(sort_mem + kClusterCounts);             // [1024 I]: key, position
   __shared__ uint32_t total[2][kMaxBins], first[kMaxBins], warp_total[kMaxBins / 32];
@@ -244,8 +243,6 @@ __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const 
   const uint32_t rank = blocks > 1 ? tc::cluster_ctarank() : 0;
   constexpr int kHeld = kClusterThreads * I;
   const int begin = warp * 32 * I + lane;  // this lane's first entry in the block
-  chain_enter();
-  let_next_start();
   uint32_t k[I], p[I], place[I];
 #pragma unroll
   for (int r = 0; r < I; ++r) {
@@ -340,37 +337,69 @@ __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const 
   if (blocks > 1) tc::cluster_sync();  // no block reads the counts of one that is gone
 }
 
+template <int I>
+__global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const void *tokens, int32_t dtype, int64_t vocab,
+                                                                          int32_t n, int passes, int bits, int blocks, uint2 *out) {
+  extern __shared__ __align__(16) char sort_mem[];
+  chain_enter();
+  let_next_start();
+  cluster_sort<I>(sort_mem, tokens, dtype, vocab, n, passes, bits, blocks, out);
+}
+
 // --------------------------------------------------------------------------------- zero ---
 // Zeros in the rows that no token names.  A block has `rows` rows: it looks through all tokens for them, a
 // flag for each in shared memory, and then writes.  Runs beside the sort.
 constexpr int kZeroThreads = 1024, kZeroMaxRows = 8192;
+struct Zero {
+  const void *tokens;
+  int32_t dtype, n, vocab, dim, rows;
+  int64_t ldd;
+};
 template <class T>
-__global__ void __launch_bounds__(kZeroThreads) zero_kernel(const void *tokens, int32_t dtype, int32_t n, int32_t vocab, int32_t dim,
-                                                            int32_t rows, T *dst, int64_t ldd, int beside_sort) {
-  __shared__ uint8_t named[kZeroMaxRows];
+__device__ __forceinline__ void zero_rows(const Zero &z, uint8_t *named, int block, T *dst) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int first = blockIdx.x * rows, count = min(rows, vocab - first);
+  const int first = block * z.rows, count = min(z.rows, z.vocab - first);
   for (int i = threadIdx.x; i < count; i += kZeroThreads) named[i] = 0;
-  if (!beside_sort) chain_enter();
   __syncthreads();
 #pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += kZeroThreads) {
-    const int64_t t = load_index(tokens, dtype, i) - first;
+  for (int i = threadIdx.x; i < z.n; i += kZeroThreads) {
+    const int64_t t = load_index(z.tokens, z.dtype, i) - first;
     if (t >= 0 && t < count) named[t] = 1;
   }
   __syncthreads();
   for (int r = warp; r < count; r += kZeroThreads / 32) {
     if (named[r]) continue;
-    T *row = dst + (int64_t)(first + r) * ldd;
-    const int head = min(dim, (int)((16 - reinterpret_cast<uintptr_t>(row) % 16) % 16 / sizeof(T)));  // up to a multiple of 16 bytes
-    const int chunks = (dim - head) * (int)sizeof(T) / 16, rest = head + chunks * (16 / (int)sizeof(T));
+    T *row = dst + (first + r) * z.ldd;
+    const int head = min(z.dim, (int)((16 - reinterpret_cast<uintptr_t>(row) % 16) % 16 / sizeof(T)));  // up to a multiple of 16 bytes
+    const int chunks = (z.dim - head) * (int)sizeof(T) / 16, rest = head + chunks * (16 / (int)sizeof(T));
     if (lane < head) row[lane] = T(0.f);
     uint4 *to = reinterpret_cast<uint4 *>(row + head);
     for (int c = lane; c < chunks; c += 32) __stcs(to + c, make_uint4(0, 0, 0, 0));
-    if (rest + lane < dim) row[rest + lane] = T(0.f);
+    if (rest + lane < z.dim) row[rest + lane] = T(0.f);
   }
+}
+template <class T>
+__global__ void __launch_bounds__(kZeroThreads) zero_kernel(const __grid_constant__ Zero z, T *dst, int beside_sort) {
+  __shared__ uint8_t named[kZeroMaxRows];
+  if (!beside_sort) chain_enter();
+  zero_rows(z, named, blockIdx.x, dst);
   if (beside_sort) chain_enter();
 }
+
+// Both in one launch, for what one block sorts in one round: block 0 sorts, the others zero.  A gradient of so
+// few tokens is bound by its launches (one token into 1000 x 64: 15 us against 19 in two launches, 1023 into
+// 32000 x 768 21.0 against 21.9).
+template <class T>
+__global__ void __launch_bounds__(kClusterThreads, 1) sort_zero_kernel(const __grid_constant__ Zero z, T *dst, int passes, int bits,
+                                                                       uint2 *out) {
+  extern __shared__ __align__(16) char sort_mem[];
+  chain_enter();
+  if (blockIdx.x == 0)
+    cluster_sort<1>(sort_mem, z.tokens, z.dtype, z.vocab, z.n, passes, bits, 1, out);
+  else
+    zero_rows(z, reinterpret_cast<uint8_t *>(sort_mem), blockIdx.x - 1, dst);
+}
+static_assert(kZeroThreads == kClusterThreads && kZeroMaxRows <= (int)kClusterCounts, "one launch for both");
 
 // --------------------------------------------------------------------------------- walk ---
 struct Walk {
@@ -667,7 +696,21 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
   while (((int64_t)1 << bits) <= p->vocab) ++bits;
   const int passes = (bits + 8) / 9, digit = (bits + passes - 1) / passes;
   int at = 0;
-  if (num_tokens > 0 && num_tokens <= (int64_t)kMaxClusterBlocks * kClusterThreads * kMaxClusterItems) {
+  // zeroing: a block on each SM that the sort leaves
+  const int64_t want = std::max(1, p->num_sms - kMaxClusterBlocks), rows = (p->vocab + want - 1) / want;
+  const Zero z{tokens,           token_dtype,     (int32_t)num_tokens, (int32_t)p->vocab,
+               (int32_t)p->dim,  (int32_t)std::min<int64_t>(rows, kZeroMaxRows), ldd};
+  const int64_t zero_blocks = (p->vocab + z.rows - 1) / z.rows;
+  const bool fused = !accumulate && num_tokens > 0 && num_tokens <= kClusterThreads;
+  auto with_out = [&](auto f) {
+    return table_grad_dtype == DION_DTYPE_FP32 ? f(static_cast<float *>(table_grad)) : f(static_cast<__nv_bfloat16 *>(table_grad));
+  };
+  if (fused) {
+    e = with_out([&](auto *dst) {
+      return launch(sort_zero_kernel<std::remove_pointer_t<decltype(dst)>>, 1 + zero_blocks, kClusterThreads,
+                    kClusterCounts + sizeof(uint2) * kClusterThreads, s, 1, z, dst, passes, digit, p->entry[0]);
+    });
+  } else if (num_tokens > 0 && num_tokens <= (int64_t)kMaxClusterBlocks * kClusterThreads * kMaxClusterItems) {
     const int64_t rounds = (num_tokens + kClusterThreads - 1) / kClusterThreads;
     const int blocks = rounds <= kOneBlockRounds ? 1 : kMaxClusterBlocks;
     const int64_t items = (rounds + blocks - 1) / blocks;
@@ -704,17 +747,11 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
   w.n = (int32_t)num_tokens, w.vocab = (int32_t)p->vocab, w.dim = (int32_t)p->dim, w.slabs = (int32_t)p->slabs;
   w.ldg = ldg, w.ldd = ldd, w.scale = scale;
   w.head = p->head, w.tail = p->tail, w.head_row = p->head_row, w.tail_row = p->tail_row;
-  if (!accumulate) {
-    // a block on each SM that the sort leaves
-    const int64_t want = std::max(1, p->num_sms - kMaxClusterBlocks), rows = (p->vocab + want - 1) / want;
-    const int32_t per = (int32_t)std::min<int64_t>(rows, kZeroMaxRows);
-    const int64_t grid = (p->vocab + per - 1) / per;
-    const int beside = num_tokens > 0;
-    e = table_grad_dtype == DION_DTYPE_FP32
-            ? launch(zero_kernel<float>, grid, kZeroThreads, 0, s, 1, tokens, token_dtype, w.n, w.vocab, w.dim, per,
-                     static_cast<float *>(table_grad), ldd, beside)
-            : launch(zero_kernel<__nv_bfloat16>, grid, kZeroThreads, 0, s, 1, tokens, token_dtype, w.n, w.vocab, w.dim, per,
-                     static_cast<__nv_bfloat16 *>(table_grad), ldd, beside);
+  if (!accumulate && !fused) {
+    e = with_out([&](auto *dst) {
+      return launch(zero_kernel<std::remove_pointer_t<decltype(dst)>>, zero_blocks, kZeroThreads, 0, s, 1, z, dst,
+                    (int)(num_tokens > 0));
+    });
     if (e != cudaSuccess) return DION_ERR_CUDA;
   }
   if (num_tokens == 0) return DION_OK;
@@ -732,7 +769,7 @@ dion_status dion_embed_gradient(dion_embed_plan *p, const void *tokens, int32_t 
       return accumulate ? launch(walk_kernel<TG, TD, V, true>, blocks, kWalkThreads, 0, s, 1, w, g, d)
                         : launch(walk_kernel<TG, TD, V, false>, blocks, kWalkThreads, 0, s, 1, w, g, d);
     });
-    if (r != cudaSuccess) return r;
+    if (r != cudaSuccess || w.parts == 1) return r;
     return accumulate ? launch(join_kernel<TD, true>, w.parts, kJoinThreads, 0, s, 1, w, d)
                       : launch(join_kernel<TD, false>, w.parts, kJoinThreads, 0, s, 1, w, d);
   });
