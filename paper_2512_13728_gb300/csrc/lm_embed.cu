@@ -56,7 +56,8 @@ __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.
 // 48 us with one, 38 with two, 44 with four; of 1024 bf16 elements 23, 17 and 15 us).
 template <class TE, int V>
 constexpr int kLookupTokens = 64 / (8 / V * (int)sizeof(Raw<TE, V>));
-// A warp takes a slab of 256 columns of that many tokens; V elements per access.
+// A warp takes a slab of 256 columns of that many tokens; V elements per access.  Bound by memory: 32768 rows
+// of 2048 from a table of 50001 in fp32 to bf16 in 37 us, 5.8 TB/s of the distinct rows and the output.
 template <class TE, class TO, int V>
 __global__ void __launch_bounds__(256) lookup_kernel(const void *tokens, int32_t token_dtype, int64_t num_tokens, const TE *table,
                                                      int64_t ldt, int64_t vocab, int dim, int slabs, float scale, TO *out,
@@ -219,6 +220,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const uint2 *en
 // 1024 I), warp w of it 32 I of them in I rounds of 32.  A pass counts the digits of each warp, adds up
 // the counts over warps and (through distributed shared memory) over blocks, and writes each entry
 // to its place in the block that holds it next; the last pass writes to global memory.
+// Bound by the passes' barriers and shared memory, beside the zeroing for which it leaves all SMs but
+// eight: 32768 tokens over 50001 rows in 16 us, 1023 in 5.6.
 constexpr int kClusterThreads = 1024;
 constexpr int kClusterWarps = kClusterThreads / 32;
 constexpr int kMaxClusterItems = 16, kMaxClusterBlocks = 8;
@@ -348,7 +351,8 @@ __global__ void __launch_bounds__(kClusterThreads, 1) sort_cluster_kernel(const 
 
 // --------------------------------------------------------------------------------- zero ---
 // Zeros in the rows that no token names.  A block has `rows` rows: it looks through all tokens for them, a
-// flag for each in shared memory, and then writes.  Runs beside the sort.
+// flag for each in shared memory, and then writes.  Runs beside the sort.  Bound by memory's rate for
+// writes alone: what 32768 tokens leave of 50001 x 2048 fp32 in 58 us.
 constexpr int kZeroThreads = 1024, kZeroMaxRows = 8192;
 struct Zero {
   const void *tokens;
@@ -370,7 +374,8 @@ __device__ __forceinline__ void zero_rows(const Zero &z, uint8_t *named, int blo
   for (int r = warp; r < count; r += kZeroThreads / 32) {
     if (named[r]) continue;
     T *row = dst + (first + r) * z.ldd;
-    const int head = min(z.dim, (int)((16 - reinterpret_cast<uintptr_t>(row) % 16) % 16 / sizeof(T)));  // up to a multiple of 16 bytes
+    // up to a multiple of 16 bytes
+    const int head = min(z.dim, (int)((16 - reinterpret_cast<uintptr_t>(row) % 16) % 16 / sizeof(T)));
     const int chunks = (z.dim - head) * (int)sizeof(T) / 16, rest = head + chunks * (16 / (int)sizeof(T));
     if (lane < head) row[lane] = T(0.f);
     uint4 *to = reinterpret_cast<uint4 *>(row + head);
@@ -411,7 +416,10 @@ struct Walk {
   int32_t *head_row, *tail_row;
 };
 
-// One warp: a part of the entries, a slab of columns.  ACC: added to dst instead of written.
+// One warp: a part of the entries, a slab of columns.  ACC: added to dst instead of written.  Each gradient
+// row is read once and each row of dst written once, so it is bound by memory: 32768 bf16 rows of 2048 in 32 us,
+// 5.3 TB/s.  Rows of odd length are read by single elements, four rows on their way instead of eight, at a third
+// of that rate (38440 rows of 771 in 44 us).
 template <class TG, class TD, int V, bool ACC>
 __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_constant__ Walk w, const TG *grad, TD *dst) {
   constexpr int C = 8 / V;

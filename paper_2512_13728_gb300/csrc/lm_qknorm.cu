@@ -8,9 +8,8 @@
 // halves, with angle 0), so a rotation never leaves a lane; the mean is a shuffle sum over the group.
 // A warp keeps to one kind and a few of its heads and goes over tokens (blocks of tokens, where the heads of
 // one do not fill a warp): it computes a token's sines and cosines once, and holds the weights and the
-// sums of their gradients in registers.  What it reads runs
-// ahead of it through a ring of asynchronous copies in shared memory, of which every lane reads only what
-// it copied itself.
+// sums of their gradients in registers.  What it reads runs ahead of it through a ring of asynchronous
+// copies in shared memory, of which every lane reads only what it copied itself.
 #include "lm_common.cuh"
 #include "tc_common.cuh"
 
@@ -416,6 +415,11 @@ __device__ __forceinline__ void wait_copies() {
 }
 
 // ------------------------------------------------------------------------------ forward ---
+// Reads and writes each head once; bound by memory, close behind by instructions: 32 x 1024 tokens of 16 + 16 heads
+// of 128 in bf16 87 us, 6.2 TB/s.  A lane's 16 elements take four packed products each way for the rotation
+// with the weights multiplied into the sines and cosines once a token.  Heads of other widths leave lanes
+// of a group idle (80 elements: 5 of 8) and are bound by instructions: 6 x 6081 tokens of 4 + 2 heads of 80 in
+// 43 us, 1.6 TB/s.  One token of 16 sequences: 4.3 us of the GPU's time.
 template <class L, bool MULTI>
 __global__ void __launch_bounds__(kThreads, forward_blocks(L::kPairs)) forward_kernel(const __grid_constant__ Args A) {
   using T = typename L::T;
@@ -491,6 +495,11 @@ __global__ void __launch_bounds__(kThreads, forward_blocks(L::kPairs)) forward_k
 }
 
 // ----------------------------------------------------------------------------- backward ---
+// Reads x and g once, writes dx once, and adds up dw in registers over all of a warp's tokens: the weights'
+// gradient costs no memory but a block's sums at the end.  Two means per head (of x^2 and of w gu x) share one
+// round of shuffles.  Bound by memory: 32 x 1024 tokens of 16 + 16 heads of 128 in bf16 134 us with the sums of
+// dw, 6.0 TB/s; a few thousand tokens by their latency (3 x 701 of 12 + 12 heads of 64 in fp32: 9.5 us, and 4.0
+// for the sums).
 template <class L, bool MULTI>
 __global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward_kernel(const __grid_constant__ Args A) {
   using T = typename L::T;
@@ -614,7 +623,8 @@ __global__ void __launch_bounds__(kThreads, backward_blocks(L::kPairs)) backward
   }
 }
 
-// dw from the blocks' sums: a block per 32 columns, whose warps take the rows in turn; fixed order.
+// dw from the blocks' sums: a block per 32 columns, whose warps take the rows in turn; fixed order.  Bound by
+// latency: 456 blocks' sums of 2 x 128 in 4 us.
 constexpr int kSumThreads = 1024;
 __global__ void __launch_bounds__(kSumThreads) sum_weights_kernel(const float *partial, int blocks, int dim, float *dwq, float *dwk) {
   __shared__ float red[kSumThreads / 32][33];
