@@ -487,7 +487,7 @@ __device__ __forceinline__ bool wait_stats(uint64_t *bar, uint32_t parity) {
 // (which brings the row's entries and takes its statistics) and the teacher of row n - 1 (which now
 // writes that row's entries over what the workers wrote there).  So a teacher has `teachers` - 1 rows of
 // time for its loads and softmax, and a worker meets one barrier per row.
-// Bound by memory with one softmax: 8192 rows of 50001 bf16 logits with 128 entries in 261 us, 6.3 TB/s.  With
+// Bound by memory with one softmax: 8192 rows of 50001 bf16 logits with 128 entries in 259 us, 6.3 TB/s.  With
 // two (both terms, T not 1) each bf16 logit takes four exponentials instead of two, and a row's two phases
 // (sums, gradient) no longer hide behind the other blocks' copies: 4256 rows of 63897 in 234 us, 4.7 TB/s.
 // (Sums begun on a row's first quarter while the rest is on its way were slower: 288 us for 262.)
@@ -623,7 +623,9 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_kernel(const __grid_cons
         auto put = [&] {
           float v[N];
           gradient(*place, v);
-          store_vec<T, N>(reinterpret_cast<T *>(to), v);
+          uint4 raw;
+          store_vec<T, N>(reinterpret_cast<T *>(&raw), v);
+          __stcs(to, raw);  // the next rows' logits stay in L2 instead (8192 rows of 50001 bf16: 259 us, 263 without)
         };
         if (zeros) {
           for (; c < both_hi; c += threads, place += threads, from += threads, to += threads) {
