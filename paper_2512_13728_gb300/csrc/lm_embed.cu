@@ -418,8 +418,9 @@ struct Walk {
 
 // One warp: a part of the entries, a slab of columns.  ACC: added to dst instead of written.  Each gradient
 // row is read once and each row of dst written once, so it is bound by memory: 32768 bf16 rows of 2048 in 32 us,
-// 5.3 TB/s.  Rows of odd length are read by single elements, four rows on their way instead of eight, at a third
-// of that rate (38440 rows of 771 in 44 us).
+// 5.3 TB/s.  Rows of odd length are read by single elements, with half as many bytes on their way.  Every load of
+// a batch is unconditional, so that all are on their way together (a call of 38440 bf16 rows of 771: 58 us,
+// 73 with loads under conditions; 18829 of 2050: 42 and 57).
 template <class TG, class TD, int V, bool ACC>
 __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_constant__ Walk w, const TG *grad, TD *dst) {
   constexpr int C = 8 / V;
@@ -434,7 +435,10 @@ __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_cons
   const int first = (int)w.entry[j0].x;
   const int begun = j0 > 0 && first < w.vocab && (int)w.entry[j0 - 1].x == first ? first : -1;
   const int64_t partial = (int64_t)unit * kSlab + lane * V;  // where the part's sums go
-  const TG *src = grad + c0;
+  // (columns beyond the row are read as its last ones and not written)
+  const TG *src[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) src[c] = grad + min(c0 + c * 32 * V, w.dim - V);
   TD *out = dst + c0;
   float acc[C][V];
 #pragma unroll
@@ -463,17 +467,13 @@ __global__ void __launch_bounds__(kWalkThreads, 4) walk_kernel(const __grid_cons
     // 32 entries' keys and positions, one per lane
     const uint2 mine = j + lane < j1 ? w.entry[j + lane] : make_uint2(w.vocab, 0);
     for (int e0 = 0; e0 < 32 && e0 < j1 - j; e0 += U) {
+      if ((int)__shfl_sync(0xffffffffu, mine.x, e0) >= w.vocab) break;  // entries outside the table come last
       Raw<TG, V> raw[U][C];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int at = (int)__shfl_sync(0xffffffffu, mine.y, e0 + u), k = (int)__shfl_sync(0xffffffffu, mine.x, e0 + u);
-        const TG *from = src + at * w.ldg;
+        const int64_t at = (int64_t)__shfl_sync(0xffffffffu, mine.y, e0 + u) * w.ldg;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-#pragma unroll
-          for (uint32_t &x : raw[u][c].w) x = 0;
-          if (k < w.vocab && c0 + c * 32 * V < w.dim) raw[u][c].load(from + c * 32 * V);
-        }
+        for (int c = 0; c < C; ++c) raw[u][c].load(src[c] + at);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
