@@ -80,6 +80,7 @@ struct Args {
   int32_t steps;      // of a block, what a warp takes (a batch) at most
   int32_t dim, half;  // half = rotary / 2
   int32_t group;      // lanes per head
+  bool multi;         // whether blocks have several tokens
   float eps;
   const void *pos;
   int64_t pos_sb;
@@ -419,7 +420,7 @@ __device__ __forceinline__ void wait_copies() {
 // of 128 in bf16 87 us, 6.2 TB/s.  A lane's 16 elements take four packed products each way for the rotation
 // with the weights multiplied into the sines and cosines once a token.  Heads of other widths leave lanes
 // of a group idle (80 elements: 5 of 8) and are bound by instructions: 6 x 6081 tokens of 4 + 2 heads of 80 in
-// 43 us, 1.6 TB/s.  One token of 16 sequences: 4.3 us of the GPU's time.
+// 39 us, 1.8 TB/s.  One token of 16 sequences: 4.3 us of the GPU's time.
 template <class L, bool MULTI>
 __global__ void __launch_bounds__(kThreads, forward_blocks(L::kPairs)) forward_kernel(const __grid_constant__ Args A) {
   using T = typename L::T;
@@ -680,19 +681,18 @@ dion_status check_shape(const dion_qknorm_plan *p, const dion_qk_shape *s) {
   return DION_OK;
 }
 
-// Tokens of a block for `heads` heads of which a warp takes `groups` at a time: the number with the least
-// instructions per token, of about 170 for a step (300 where each step is of other tokens), 50 for each 32 of
-// the block's angles, 80 for the block.  Blocks of several tokens leave every warp one at least.  (71829
-// tokens of 3 + 3 heads of 96 in bf16: 91 us token by token, 68 in blocks of four; 63915 tokens of 12 + 3 heads
-// of 32: 67 and 38 us.)
+// Instructions per token in blocks of n tokens, for `heads` heads of which a warp takes `groups` at a time:
+// about 170 for a step, 300 in the kernel where each step may be of other tokens, 50 for each 32 of the
+// block's angles, 80 for the block.
+double block_cost(int n, bool multi, int heads, int groups, int pairs) {
+  const int steps = (n * heads + groups - 1) / groups;
+  return (double)(steps * (multi ? 300 : 170) + (n * pairs + 31) / 32 * 50 + 80) / n;
+}
+// The tokens of a block with the least of them, up to `most`; each of `warps` warps is left one block at least.
 int block_tokens(int heads, int groups, int pairs, int most, int64_t all, int64_t warps) {
-  auto cost = [&](int n) {
-    const int steps = (n * heads + groups - 1) / groups;
-    return (double)(steps * (n > 1 ? 300 : 170) + (n * pairs + 31) / 32 * 50 + 80) / n;
-  };
   int best = 1;
   for (int n = 2; heads > 0 && n <= most && (all + n - 1) / n >= warps; ++n)
-    if (cost(n) < cost(best)) best = n;
+    if (block_cost(n, true, heads, groups, pairs) < block_cost(best, true, heads, groups, pairs)) best = n;
   return best;
 }
 
@@ -708,11 +708,23 @@ Args make_args(const dion_qknorm_plan *p, const dion_qk_shape *s, int pairs, int
   A.group = 1;
   while (A.group * pairs < p->head_dim / 2) A.group *= 2;
   const int groups = 32 / A.group, most = std::min(kMaxBlockTokens, pairs * 64 / p->head_dim);
+  // blocks of several tokens, where both kinds together gain (71829 tokens of 3 + 3 heads of 96 in bf16: 91 us
+  // token by token, 62 in blocks of four; 63915 tokens of 12 + 3 heads of 32: 67 and 38 us)
+  int tokens[2];
+  double single = 0, several = 0;
+  for (int i = 0; i < 2; ++i) {
+    const int heads = i ? s->kv_heads : s->heads, half = p->head_dim / 2;
+    tokens[i] = block_tokens(heads, groups, half, most, A.all, resident * kWarps);
+    if (heads == 0) continue;
+    single += block_cost(1, false, heads, groups, half);
+    several += block_cost(tokens[i], true, heads, groups, half);
+  }
+  const bool multi = A.multi = several < single;
   int64_t cycle = 0, work = 0;
   for (int i = 0; i < 2; ++i) {
     Kind &K = A.kind[i];
     K.heads = i ? s->kv_heads : s->heads;
-    K.tokens = block_tokens(K.heads, groups, p->head_dim / 2, most, A.all, resident * kWarps);
+    K.tokens = multi ? tokens[i] : 1;
     K.steps = (K.tokens * K.heads + groups - 1) / groups;
     K.blocks = (int32_t)(((int64_t)A.all + K.tokens - 1) / K.tokens);
     K.by_heads = FastDiv::of((uint32_t)std::max(K.heads, 1));
@@ -826,7 +838,7 @@ dion_status dion_qknorm_forward(dion_qknorm_plan *p, const dion_qk_shape *s, con
   int64_t blocks = 0;
   Args A = make_args(p, s, v == 8 ? 8 : 4, (int64_t)p->num_sms * forward_blocks(v == 8 ? 8 : 4), &blocks);
   A.q = h[0], A.k = h[1], A.oq = h[2], A.ok = h[3], A.wq = wq, A.wk = wk;
-  const bool multi = A.kind[0].tokens > 1 || A.kind[1].tokens > 1;
+  const bool multi = A.multi;
   const cudaError_t e = with_lane(s->dtype, v, heads_in_pieces(p, s, h, 4), p->interleaved, [&](auto lane) {
     using L = typename decltype(lane)::type;
     return launch(multi ? forward_kernel<L, true> : forward_kernel<L, false>, blocks, kThreads, 0,
@@ -862,7 +874,7 @@ dion_status dion_qknorm_backward(dion_qknorm_plan *p, const dion_qk_shape *s, co
   Args A = make_args(p, s, v == 8 ? 8 : 4, (int64_t)p->num_sms * backward_blocks(v == 8 ? 8 : 4), &blocks);
   A.gq = h[0], A.gk = h[1], A.q = h[2], A.k = h[3], A.oq = h[4], A.ok = h[5];
   A.wq = wq, A.wk = wk, A.partial = dwq || dwk ? p->partial : nullptr;
-  const bool multi = A.kind[0].tokens > 1 || A.kind[1].tokens > 1;
+  const bool multi = A.multi;
   cudaError_t e = with_lane(s->dtype, v, heads_in_pieces(p, s, h, 6), p->interleaved, [&](auto lane) {
     using L = typename decltype(lane)::type;
     return launch(multi ? backward_kernel<L, true> : backward_kernel<L, false>, blocks, kThreads, 0, cs, 1, A);
