@@ -27,7 +27,9 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxWorkers = 12, kMaxTeachers = 3;  // warps of the gradient's blocks
 constexpr int kShortThreads = 256;
-constexpr int kShortChunks = 512;                   // of a row that a warp takes alone (8 KB)
+// Of a row that a warp takes alone: 8 KB with gradient, 16 KB without (8192 rows of 4201 bf16 logits: 20 us, 35
+// with a block per row; 2813 of 16000, 2000 chunks: 24 and 19).
+constexpr int kShortChunks = 512, kShortLossChunks = 1024;
 constexpr int kGradThreads = 512;                   // of a block; two blocks per SM
 constexpr int kLossThreads = 256;
 constexpr int kMaxCluster = 8;
@@ -687,7 +689,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_kernel(const __grid_cons
 
 // ----------------------------------------------------------------------------- short rows ---
 // A warp per row, with or without gradient: the row in its shared memory (gradient) or straight from
-// global memory, no barriers.  For rows of up to kShortChunks chunks, of which a block would spend its time
+// global memory, no barriers.  For rows of few chunks, of which a block would spend its time
 // waiting for the teacher's entries.  (8192 rows of 1000 bf16 logits with 64 entries: 12 us the loss, 17 us with
 // gradient, of which about 10 are the call's.)
 template <class T, bool GRAD, bool TWO>
@@ -861,7 +863,7 @@ dion_status enqueue_loss(const dion_distill *d, float *loss, cudaStream_t s) {
   if (sms == 0) return DION_ERR_CUDA;
   Args A = make_args(d, loss);
   const int64_t chunks = row_chunks(d);
-  if (chunks <= kShortChunks && d->rows > 2 * sms) return enqueue_short<false>(A, chunks, s);
+  if (chunks <= kShortLossChunks && d->rows > 2 * sms) return enqueue_short<false>(A, chunks, s);
   A.cluster = 1;  // more blocks per row while the rows leave SMs idle and a thread has more than one round of chunks
   while (A.cluster < kMaxCluster && d->rows * A.cluster * 2 <= sms && chunks / A.cluster > 4 * kLossThreads) A.cluster *= 2;
   A.part = part_of(chunks, A.cluster);

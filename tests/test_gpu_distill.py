@@ -188,6 +188,28 @@ def test_masks(cd, dtype, v):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("v,k,pad,offset", [(600, 8, 0, 0), (2001, 200, 3, 1), (4100, 5, 0, 3), (8111, 40, 1, 0)])
+def test_many_rows_of_few_logits(cd, v, k, pad, offset, dtype):
+    """Every kind of row among many: masked, without entries, without label, left out, entries that come twice."""
+    z, ids, t, labels, w, _ = make(801, v, k, dtype, pad=pad, offset=offset)
+    kind = torch.arange(801, device="cuda") % 9
+    ids[kind == 0] = torch.arange(k, device="cuda") * 2
+    z[:, 1::2] = torch.where((kind == 0)[:, None], torch.full_like(z[:, 1::2], -INF), z[:, 1::2])
+    ids[kind == 1] = -1
+    t[kind == 2] = -INF
+    labels[(kind == 2) | (kind == 3)] = -1
+    ids[:, 0] = torch.where(kind == 4, ids[:, k - 1], ids[:, 0])
+    labels[kind == 4] = ids[kind == 4, 0].to(labels.dtype)
+    w[kind == 5] = 0
+    for T, hard in ((2.0, 0.0), (1.5, 0.4), (1.0, 1.0)):
+        rows = kind != 0 if hard > 0 else slice(None)  # a label in a masked column: an infinite loss
+        l, g = cd.distill_loss_grad(z, ids, t, T, labels, hard, w)
+        assert (g[kind == 5] == 0).all() and (l[kind == 5] == 0).all()
+        check(cd, z[rows], ids[rows], t[rows], T, labels[rows], hard, w[rows])
+
+
+@pytest.mark.gpu
 def test_without_weights_entries_or_rows(cd):
     z, ids, t, labels, w, _ = make(6, 500, 4, FP32)
     w.fill_(1.0)
