@@ -27,7 +27,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxWorkers = 12, kMaxTeachers = 3;  // warps of the gradient's blocks
 constexpr int kShortThreads = 256;
-// Of a row that a warp takes alone: 8 KB with gradient, 16 KB without (8192 rows of 4201 bf16 logits: 20 us, 35
+// Of a row that a warp takes alone: 8 KB with gradient, 16 KB without (8192 rows of 4201 bf16 logits: 18 us, 35
 // with a block per row; 2813 of 16000, 2000 chunks: 24 and 19).
 constexpr int kShortChunks = 512, kShortLossChunks = 1024;
 constexpr int kGradThreads = 512;                   // of a block; two blocks per SM
@@ -193,6 +193,44 @@ struct Row {
   }
 };
 
+// Thread tid's statistics of the block's chunks of a row, straight from global memory: four loads on their
+// way at a time, all of them unconditional (a chunk beyond the last is read as the last and counts nothing).
+// The edges' elements go to the first threads, one each.
+template <class T, bool TWO>
+__device__ __forceinline__ Stats sum_row(const Row<T> &r, int tid, int threads, float scale) {
+  constexpr int N = 16 / sizeof(T);
+  Stats s{-INFINITY, 0.f, 0.f};
+  if (tid < 2 * N) {
+    const bool last = tid >= N, there = last ? r.whole_hi < r.hi && r.hi > r.whole_lo : r.lo < r.whole_lo && r.lo < r.hi;
+    const int j = r.column(last ? r.hi - 1 : r.lo) + tid % N;
+    if (there && j >= 0 && j < r.vocab) {
+      const float z = load_one(r.z + j);
+      s.m = z == z ? z : -INFINITY;
+      s.s = s.s1 = z == -INFINITY ? 0.f : fabsf(z) < INFINITY ? 1.f : NAN;
+    }
+  }
+  int c = r.first(tid, threads);
+  if (c < r.whole_lo) c += threads;
+  const uint4 *from = r.at(c);
+  for (; c + 3 * threads < r.whole_hi; c += 4 * threads, from += 4 * threads) {
+    Chunk<T> v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u].raw = __ldcs(from + u * threads);
+    take<T, 4, TWO>(v, s, scale);
+  }
+  if (c < r.whole_hi) {
+    constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;  // -infinity
+    Chunk<T> v[3];
+#pragma unroll
+    for (int u = 0; u < 3; ++u) v[u].raw = __ldcs(from + min(u * threads, r.whole_hi - 1 - c));
+#pragma unroll
+    for (int u = 1; u < 3; ++u)
+      if (c + u * threads >= r.whole_hi) v[u].raw = make_uint4(kNone, kNone, kNone, kNone);
+    take<T, 3, TWO>(v, s, scale);
+  }
+  return s;
+}
+
 // The teacher's entries of a row, and the label as one more, in shared memory; one warp's work.
 struct Entries {
   int32_t *col;  // column, -1: absent
@@ -342,7 +380,7 @@ __device__ __forceinline__ void send(const Stats &s, Stats *blocks, int to, int 
 }
 // --------------------------------------------------------------------------------- loss ---
 // One row per cluster, straight from global memory; the last warp has the teacher's entries.  Bound by
-// memory: 4096 rows of 50001 fp32 logits with 64 entries in 117 us, 7.0 TB/s (a row's loads have no stores
+// memory: 4096 rows of 50001 fp32 logits with 64 entries in 115 us, 7.1 TB/s (a row's loads have no stores
 // between them, which a plain copy has).  Up to 16 rows or so it is the launch and one row's latency: 9 rows
 // of 32000 bf16 logits in 4.7 us of the GPU's time.
 template <class T, bool TWO>
@@ -370,30 +408,7 @@ __global__ void __launch_bounds__(kLossThreads, 6) loss_kernel(const __grid_cons
     }
   } else {
     const Row<T> r(A, row, rank);
-    Stats s{-INFINITY, 0.f, 0.f};
-    int c = r.first(tid, threads);
-    Chunk<T> one[1];
-    if (c < r.whole_lo && c < r.hi) {
-      one[0].raw = r.edge(c);
-      take<T, 1, TWO>(one, s, A.c);
-      c += threads;
-    }
-    const uint4 *from = r.at(c);
-    for (; c + 3 * threads < r.whole_hi; c += 4 * threads, from += 4 * threads) {
-      Chunk<T> v[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[u].raw = __ldcs(from + u * threads);
-      take<T, 4, TWO>(v, s, A.c);
-    }
-    for (; c < r.whole_hi; c += threads, from += threads) {
-      one[0].raw = __ldcs(from);
-      take<T, 1, TWO>(one, s, A.c);
-    }
-    if (c < r.hi) {
-      one[0].raw = r.edge(c);
-      take<T, 1, TWO>(one, s, A.c);
-    }
-    s = merge_lanes<TWO>(s, A.c);
+    const Stats s = merge_lanes<TWO>(sum_row<T, TWO>(r, tid, threads, A.c), A.c);
     if ((tid & 31) == 0) warp_stats[warp] = s;
   }
   __syncthreads();
@@ -690,7 +705,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_kernel(const __grid_cons
 // ----------------------------------------------------------------------------- short rows ---
 // A warp per row, with or without gradient: the row in its shared memory (gradient) or straight from
 // global memory, no barriers.  For rows of few chunks, of which a block would spend its time
-// waiting for the teacher's entries.  (8192 rows of 1000 bf16 logits with 64 entries: 12 us the loss, 17 us with
+// waiting for the teacher's entries.  (8192 rows of 1000 bf16 logits with 64 entries: 11 us the loss, 16 us with
 // gradient, of which about 10 are the call's.)
 template <class T, bool GRAD, bool TWO>
 __global__ void __launch_bounds__(kShortThreads, 4) short_kernel(const __grid_constant__ Args A) {
@@ -729,19 +744,22 @@ __global__ void __launch_bounds__(kShortThreads, 4) short_kernel(const __grid_co
   gather_logits<T>(A, row, b, z);
   const RowTerms terms = set_entries<T>(A, row, E, b, z, label, label_logit<T>(A, row, label));
   Stats s{-INFINITY, 0.f, 0.f};
-  asm volatile("cp.async.wait_all;" ::: "memory");  // each lane reads only what it copied itself
-  auto chunk = [&](int c) { return GRAD ? mine[c] : r.whole(c) ? *r.at(c) : r.edge(c); };
-  int c = r.first(lane, 32);
-  for (; c + 96 < r.hi; c += 128) {
-    Chunk<T> v[4];
+  if constexpr (GRAD) {
+    asm volatile("cp.async.wait_all;" ::: "memory");  // each lane reads only what it copied itself
+    int c = r.first(lane, 32);
+    for (; c + 96 < r.hi; c += 128) {
+      Chunk<T> v[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u].raw = chunk(c + 32 * u);
-    take<T, 4, TWO>(v, s, A.c);
-  }
-  for (; c < r.hi; c += 32) {
-    Chunk<T> v[1];
-    v[0].raw = chunk(c);
-    take<T, 1, TWO>(v, s, A.c);
+      for (int u = 0; u < 4; ++u) v[u].raw = mine[c + 32 * u];
+      take<T, 4, TWO>(v, s, A.c);
+    }
+    for (; c < r.hi; c += 32) {
+      Chunk<T> v[1];
+      v[0].raw = mine[c];
+      take<T, 1, TWO>(v, s, A.c);
+    }
+  } else {
+    s = sum_row<T, TWO>(r, lane, 32, A.c);
   }
   s = merge_lanes<TWO>(s, A.c);
   const float loss = w * row_loss<TWO>(A, E, terms, s);
@@ -750,7 +768,7 @@ __global__ void __launch_bounds__(kShortThreads, 4) short_kernel(const __grid_co
   const Factors f = factors<TWO>(A, terms, s, w);
   const bool zeros = !terms.soft && !terms.hard;
   const bool same_place = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T)) == r.lead % N;
-  for (c = r.first(lane, 32); c < r.hi; c += 32) {
+  for (int c = r.first(lane, 32); c < r.hi; c += 32) {
     Chunk<T> x;
     x.raw = mine[c];
     float v[N];
