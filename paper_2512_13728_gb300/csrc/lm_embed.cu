@@ -53,7 +53,8 @@ __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.
 
 // ------------------------------------------------------------------------------- lookup ---
 // Tokens whose rows a warp has on their way: 16 registers of a lane (32768 rows of 2048 fp32 elements to bf16:
-// 48 us with one, 38 with two, 44 with four; of 1024 bf16 elements 23, 17 and 15 us).
+// 48 us with one, 38 with two, 44 with four; of 1024 bf16 elements 23, 17 and 15 us, 13.5 with loads that are
+// unconditional; narrower accesses gain nothing from those: 771 fp32 elements 20 us, 24 with them).
 template <class TE, int V>
 constexpr int kLookupTokens = 64 / (8 / V * (int)sizeof(Raw<TE, V>));
 // A warp takes a slab of 256 columns of that many tokens; V elements per access.  Bound by memory: 32768 rows
@@ -76,6 +77,10 @@ __global__ void __launch_bounds__(256) lookup_kernel(const void *tokens, int32_t
   for (int u = 0; u < U; ++u) {
     const int64_t t = i0 + u < num_tokens ? load_index(tokens, token_dtype, i0 + u) : -1;
     real[u] = t >= 0 && t < vocab;
+    if (C == 1) {  // without conditions, for all to be on their way together: row 0 for padding, the row's end beyond it
+      row[u][0].load(table + (real[u] ? t : 0) * ldt + min(c0, dim - V));
+      continue;
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
 #pragma unroll
